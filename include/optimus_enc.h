@@ -453,6 +453,111 @@ int enc_qkv_bwd_data_add(int M, int H, int A, const enc_bf16 *dqkv,
                          enc_bf16 *dy, void *ws, size_t ws_bytes,
                          enc_stream_t stream);
 
+/* ------------------------------------------------------------ packed sequences
+ *
+ * The paper's encoders see images of one size; encoders that take images,
+ * video and text of any size keep the micro-batch's sequences end to end,
+ * without padding.  A packed batch is `tokens` rows that hold `seqs`
+ * sequences: sequence i is rows cu_seqlens[i] .. cu_seqlens[i + 1] - 1, with
+ * int32 offsets [seqs + 1] on the device that start at 0 or later and do not
+ * decrease (a sequence may be empty).  Rows in front of the first and behind
+ * the last sequence belong to none: the attention neither reads nor writes
+ * them.  Everything else of a layer works on rows and needs no offsets.
+ *
+ * qkv rows are packed [heads + 2 kv_heads][head_dim]: queries, keys, values.
+ * Query head h reads key and value head h / (heads / kv_heads); with
+ * kv_heads = heads this is the qkv of the other entry points.  The projection
+ * that writes it is enc_qkv_fwd with 3A = (heads + 2 kv_heads) * head_dim.
+ * Limits: heads a multiple of kv_heads and at most 65536, at most 65536
+ * sequences, head_dim 64, 80 or 128. */
+
+/* [Packed block step: rotary positions in place of learned ones]
+ * Rotary positions with three axes (time, height, width).  pos [M, 3] int32
+ * holds a row's position on each axis (unused ones are not read),
+ * inv_freq [head_dim / 2] fp32 a frequency for each of a head's pairs.  Of
+ * the pairs, the first sec_t turn with the time position, the next sec_h with
+ * the height, the next sec_w with the width; pairs past sec_t + sec_h + sec_w
+ * (at most head_dim / 2) are not turned.  Pair i is elements (i, i +
+ * head_dim/2), or with interleaved = 1 (2i, 2i + 1), of every query and key
+ * head:  (a, b) -> (a cos t - b sin t, a sin t + b cos t), t = pos * inv_freq,
+ * formed in 64 bits.  Values are copied.  qkv, qkvr: [M, (heads + 2 kv_heads)
+ * * head_dim]; qkvr may be qkv itself (no other overlap). */
+int enc_rope_fwd(int M, int heads, int kv_heads, int head_dim, int sec_t, int sec_h, int sec_w, int interleaved,
+                 const enc_bf16 *qkv, const int32_t *pos, const float *inv_freq, enc_bf16 *qkvr,
+                 enc_stream_t stream);
+/* Gradient of enc_rope_fwd: the rotations undone on dq and dk, dv copied.
+ * dqkv may be dqkvr itself. */
+int enc_rope_bwd(int M, int heads, int kv_heads, int head_dim, int sec_t, int sec_h, int sec_w, int interleaved,
+                 const enc_bf16 *dqkvr, const int32_t *pos, const float *inv_freq, enc_bf16 *dqkv,
+                 enc_stream_t stream);
+
+/* [Packed block step: the work list of a batch's attention]
+ * Cuts the batch's sequences into tiles of 128 tokens, longest sequence
+ * first, into plan (enc_packed_plan_bytes), on the device.  One plan serves
+ * every attention call on a batch with these offsets, forward and backward,
+ * of any head layout; it is built once per batch.  Its contents are the
+ * library's own.  Offsets outside [0, tokens] are taken as the nearest bound
+ * and a sequence that would end before it starts as empty; where sequences
+ * overlap, results are undefined (nothing outside the tensors is touched). */
+int enc_packed_plan_bytes(int tokens, int seqs, size_t *bytes);
+int enc_packed_plan(int tokens, int seqs, const int32_t *cu_seqlens, void *plan, size_t plan_bytes,
+                    enc_stream_t stream);
+
+/* [Packed block step: self-attention within each sequence]
+ * Softmax attention of every sequence and head: P = softmax_j(q_i . k_j /
+ * sqrt(head_dim)) over the keys j of the query's sequence (with causal = 1,
+ * j <= i), o_i = sum_j P_ij v_j.  plan: enc_packed_plan for the same tokens
+ * and seqs.  qkv: [tokens, (heads + 2 kv_heads) * head_dim]; o: [tokens,
+ * heads * head_dim]; lse: [heads, tokens] fp32, natural log.  Rows of no
+ * sequence keep what o and lse held.  (With causal = 1, a non-finite key or
+ * value of a later token may still make its sequence's results NaN.) */
+int enc_attn_packed_fwd(int tokens, int seqs, int heads, int kv_heads, int head_dim, int causal, const void *plan,
+                        size_t plan_bytes, const enc_bf16 *qkv, enc_bf16 *o, float *lse, enc_stream_t stream);
+
+/* [Packed block step: backward of the self-attention within each sequence]
+ * Exact gradient of enc_attn_packed_fwd, P recomputed from lse; dK and dV are
+ * summed over the heads that share them.  dqkv: [tokens, (heads + 2 kv_heads)
+ * * head_dim]; rows of no sequence keep what dqkv held.  ws: fp32 D vector
+ * (enc_attn_packed_bwd_workspace_bytes).  No atomics, deterministic. */
+int enc_attn_packed_bwd_workspace_bytes(int tokens, int heads, size_t *bytes);
+int enc_attn_packed_bwd(int tokens, int seqs, int heads, int kv_heads, int head_dim, int causal, const void *plan,
+                        size_t plan_bytes, const enc_bf16 *qkv, const enc_bf16 *o, const float *lse,
+                        const enc_bf16 *do_, enc_bf16 *dqkv, void *ws, size_t ws_bytes, enc_stream_t stream);
+
+/* ------------------------------------------------------------ gated feed-forward
+ *
+ * A feed-forward block whose hidden activation is a gated product, in place
+ * of the GELU MLP:  [g | u] = y2 w_gu^T + b_gu,  h = act(g) * u,
+ *   out = resid + h w_2^T + b_2   (enc_mlp_down_fwd with h for g).
+ * w_gu [2F, H] holds the gate's F rows, then the up-projection's; gu is
+ * [M, 2F] with the same halves.  The down-projection's weight gradient is
+ * enc_mlp_down_bwd_weight with h for g. */
+enum enc_glu_act {
+  ENC_GLU_SILU = 0, /* act(g) = g / (1 + e^-g) */
+  ENC_GLU_GELU = 1  /* act(g) = g Phi(g) (exact erf form) */
+};
+
+/* [Gated block step: both up-projections, the activation and the product]
+ * y2 [M, H]; b_gu [2F] or NULL; h [M, F] bf16, from g and u in fp32; gu
+ * [M, 2F] or NULL (it is kept for the backward only).  ws: as for the other
+ * products, enc_linear_workspace_bytes(M, 2F, H). */
+int enc_glu_up_fwd(int M, int H, int F, int act, const enc_bf16 *y2, const enc_bf16 *w_gu, const enc_bf16 *b_gu,
+                   enc_bf16 *gu, enc_bf16 *h, void *ws, size_t ws_bytes, enc_stream_t stream);
+/* [Backward of the gated block's down-projection, product and activation]
+ * With dh = dout[M, H] w_2[H, F] (fp32) and the saved gu = [g | u]:
+ * dgu [M, 2F] = [dh u act'(g) | dh act(g)].  ws: (M, F, H). */
+int enc_glu_down_bwd_data(int M, int F, int H, int act, const enc_bf16 *dout, const enc_bf16 *w_2, const enc_bf16 *gu,
+                          enc_bf16 *dgu, void *ws, size_t ws_bytes, enc_stream_t stream);
+/* [Backward of the gated block's up-projections, input side]
+ * dy2[M, H] = dgu[M, 2F] w_gu[2F, H].  ws: (M, H, 2F). */
+int enc_glu_up_bwd_data(int M, int H, int F, const enc_bf16 *dgu, const enc_bf16 *w_gu, enc_bf16 *dy2, void *ws,
+                        size_t ws_bytes, enc_stream_t stream);
+/* [Backward of the gated block's up-projections, parameter side]
+ * dw_gu[2F, H] = dgu^T y2, db_gu[2F] (or NULL): enc_linear_bwd_weight with
+ * N = 2F, K = H, and its workspace. */
+int enc_glu_up_bwd_weight(int M, int H, int F, const enc_bf16 *dgu, const enc_bf16 *y2, float *dw_gu, float *db_gu,
+                          int accumulate, void *ws, size_t ws_bytes, enc_stream_t stream);
+
 /* ------------------------------------------------------------ whole encoder
  *
  * The encoders of the paper are ViTs (Appendix A): a patch embedding, a

@@ -108,6 +108,17 @@ _SIGS = {
     "enc_qk_norm_bwd_workspace_bytes": [_i, _i, _i, ctypes.POINTER(_sz)],
     "enc_qk_norm_bwd": [_i, _i, _i, _p, _p, _p, _p, _p, _p, _p, _p, _p, _p, _i, _p, _sz, _p],
     "enc_qkv_bwd_data_add": [_i, _i, _i, _p, _p, _p, _p, _p, _sz, _p],
+    "enc_rope_fwd": [_i, _i, _i, _i, _i, _i, _i, _i, _p, _p, _p, _p, _p],
+    "enc_rope_bwd": [_i, _i, _i, _i, _i, _i, _i, _i, _p, _p, _p, _p, _p],
+    "enc_packed_plan_bytes": [_i, _i, ctypes.POINTER(_sz)],
+    "enc_packed_plan": [_i, _i, _p, _p, _sz, _p],
+    "enc_attn_packed_fwd": [_i, _i, _i, _i, _i, _i, _p, _sz, _p, _p, _p, _p],
+    "enc_attn_packed_bwd_workspace_bytes": [_i, _i, ctypes.POINTER(_sz)],
+    "enc_attn_packed_bwd": [_i, _i, _i, _i, _i, _i, _p, _sz, _p, _p, _p, _p, _p, _p, _sz, _p],
+    "enc_glu_up_fwd": [_i, _i, _i, _i, _p, _p, _p, _p, _p, _p, _sz, _p],
+    "enc_glu_down_bwd_data": [_i, _i, _i, _i, _p, _p, _p, _p, _p, _sz, _p],
+    "enc_glu_up_bwd_data": [_i, _i, _i, _p, _p, _p, _p, _sz, _p],
+    "enc_glu_up_bwd_weight": [_i, _i, _i, _p, _p, _p, _p, _i, _p, _sz, _p],
     "enc_patch_embed_workspace_bytes": [_i, _i, _i, _i, _i, _i, _i, ctypes.POINTER(_sz)],
     "enc_patch_embed_fwd": [_i, _i, _i, _i, _i, _i, _i, _p, _p, _p, _p, _p, _p, _p, _p, _sz, _p],
     "enc_patch_embed_bwd": [_i, _i, _i, _i, _i, _i, _i, _p, _p, _p, _p, _p, _p, _i, _p, _sz, _p],
@@ -760,6 +771,159 @@ def enc_qkv_bwd_data_add(dqkv, w_qkv, addend, dy=None, ws=None, split=True, stre
     _call("enc_qkv_bwd_data_add", M, H, A3 // 3, _ptr(dqkv), _ptr(w_qkv), _ptr(addend), _ptr(dy), wp, wn,
           _stream(stream))
     return dy
+
+
+# ---------------------------------------------------------------- packed sequences
+
+def _rope(name, in_name, out_name, heads, kv_heads, head_dim, x, pos, inv_freq, sections, interleaved, y, stream):
+    M = x.shape[0]
+    width = (heads + 2 * kv_heads) * head_dim
+    _check(x, in_name, (M, width))
+    _check(pos, "pos", (M, 3), torch.int32)
+    _check(inv_freq, "inv_freq", (head_dim // 2,), torch.float32)
+    y = _out(y, out_name, (M, width), x)
+    sec_t, sec_h, sec_w = sections
+    _call(name, M, heads, kv_heads, head_dim, sec_t, sec_h, sec_w, 1 if interleaved else 0, _ptr(x), _ptr(pos),
+          _ptr(inv_freq), _ptr(y), _stream(stream))
+    return y
+
+
+def enc_rope_fwd(heads, kv_heads, head_dim, qkv, pos, inv_freq, sections, interleaved=False, qkvr=None, stream=None):
+    """qkv [M, (heads + 2 kv_heads) * head_dim] with its queries and keys turned by
+    their rows' positions: pos [M, 3] int32 (time, height, width), inv_freq
+    [head_dim / 2] fp32, sections the pairs of each axis.  qkvr may be qkv."""
+    return _rope("enc_rope_fwd", "qkv", "qkvr", heads, kv_heads, head_dim, qkv, pos, inv_freq, sections, interleaved,
+                 qkvr, stream)
+
+
+def enc_rope_bwd(heads, kv_heads, head_dim, dqkvr, pos, inv_freq, sections, interleaved=False, dqkv=None,
+                 stream=None):
+    """Gradient of enc_rope_fwd.  dqkv may be dqkvr."""
+    return _rope("enc_rope_bwd", "dqkvr", "dqkv", heads, kv_heads, head_dim, dqkvr, pos, inv_freq, sections,
+                 interleaved, dqkv, stream)
+
+
+def packed_plan_bytes(tokens, seqs):
+    n = ctypes.c_size_t()
+    _call("enc_packed_plan_bytes", tokens, seqs, ctypes.byref(n))
+    return n.value
+
+
+def enc_packed_plan(cu_seqlens, tokens, plan=None, stream=None):
+    """Work list (uint8 tensor) of a packed batch of `tokens` rows, from its
+    sequences' offsets cu_seqlens [seqs + 1] int32: built once per batch, for every
+    enc_attn_packed_* call on it."""
+    if not isinstance(cu_seqlens, torch.Tensor) or cu_seqlens.dim() != 1 or cu_seqlens.shape[0] < 2:
+        raise ValueError("cu_seqlens must be a tensor of seqs + 1 offsets")
+    seqs = cu_seqlens.shape[0] - 1
+    _check(cu_seqlens, "cu_seqlens", (seqs + 1,), torch.int32)
+    plan = _out(plan, "plan", (packed_plan_bytes(tokens, seqs),), cu_seqlens, torch.uint8)
+    _call("enc_packed_plan", tokens, seqs, _ptr(cu_seqlens), _ptr(plan), plan.numel(), _stream(stream))
+    return plan
+
+
+def attn_packed_bwd_workspace_bytes(tokens, heads):
+    n = ctypes.c_size_t()
+    _call("enc_attn_packed_bwd_workspace_bytes", tokens, heads, ctypes.byref(n))
+    return n.value
+
+
+def enc_attn_packed_fwd(seqs, heads, kv_heads, head_dim, qkv, plan, causal=False, o=None, lse=None, stream=None):
+    """Attention within the sequences of a packed batch.  Returns (o [tokens,
+    heads * head_dim], lse [heads, tokens]); rows of no sequence are left as they
+    are (uninitialised where o or lse is not given)."""
+    T = qkv.shape[0]
+    _check(qkv, "qkv", (T, (heads + 2 * kv_heads) * head_dim))
+    _check(plan, "plan", (packed_plan_bytes(T, seqs),), torch.uint8)
+    o = _out(o, "o", (T, heads * head_dim), qkv)
+    lse = _out(lse, "lse", (heads, T), qkv, torch.float32)
+    _call("enc_attn_packed_fwd", T, seqs, heads, kv_heads, head_dim, 1 if causal else 0, _ptr(plan), plan.numel(),
+          _ptr(qkv), _ptr(o), _ptr(lse), _stream(stream))
+    return o, lse
+
+
+def enc_attn_packed_bwd(seqs, heads, kv_heads, head_dim, qkv, o, lse, do, plan, causal=False, dqkv=None, ws=None,
+                        stream=None):
+    """Gradient of enc_attn_packed_fwd; rows of no sequence are left as they are."""
+    T = qkv.shape[0]
+    width = (heads + 2 * kv_heads) * head_dim
+    _check(qkv, "qkv", (T, width))
+    _check(o, "o", (T, heads * head_dim))
+    _check(lse, "lse", (heads, T), torch.float32)
+    _check(do, "do", (T, heads * head_dim))
+    _check(plan, "plan", (packed_plan_bytes(T, seqs),), torch.uint8)
+    dqkv = _out(dqkv, "dqkv", (T, width), qkv)
+    if ws is None:
+        ws = torch.empty(attn_packed_bwd_workspace_bytes(T, heads), dtype=torch.uint8, device=qkv.device)
+    _call("enc_attn_packed_bwd", T, seqs, heads, kv_heads, head_dim, 1 if causal else 0, _ptr(plan), plan.numel(),
+          _ptr(qkv), _ptr(o), _ptr(lse), _ptr(do), _ptr(dqkv), _ptr(ws), ws.numel() * ws.element_size(),
+          _stream(stream))
+    return dqkv
+
+
+# ---------------------------------------------------------------- gated feed-forward
+
+GLU_SILU, GLU_GELU = 0, 1
+
+
+def enc_glu_up_fwd(y2, w_gu, b_gu=None, act=GLU_SILU, gu=None, h=None, save=True, ws=None, split=True, stream=None):
+    """h = act(g) * u with [g | u] = y2 w_gu^T + b_gu.  Returns (gu, h); with
+    save=False gu is not written (None)."""
+    M, H = y2.shape
+    F2 = w_gu.shape[0]
+    if F2 % 2:
+        raise ValueError("w_gu rows must be 2*F")
+    _check(y2, "y2", (M, H))
+    _check(w_gu, "w_gu", (F2, H))
+    if b_gu is not None:
+        _check(b_gu, "b_gu", (F2,))
+    if save:
+        gu = _out(gu, "gu", (M, F2), y2)
+    elif gu is not None:
+        raise ValueError("gu given with save=False")
+    h = _out(h, "h", (M, F2 // 2), y2)
+    wp, wn = _gemm_ws(M, F2, H, ws, split, y2.device)
+    _call("enc_glu_up_fwd", M, H, F2 // 2, act, _ptr(y2), _ptr(w_gu), _ptr(b_gu), _ptr(gu), _ptr(h), wp, wn,
+          _stream(stream))
+    return gu, h
+
+
+def enc_glu_down_bwd_data(dout, w_2, gu, act=GLU_SILU, dgu=None, ws=None, split=True, stream=None):
+    M, H = dout.shape
+    F = w_2.shape[1]
+    _check(dout, "dout", (M, H))
+    _check(w_2, "w_2", (H, F))
+    _check(gu, "gu", (M, 2 * F))
+    dgu = _out(dgu, "dgu", (M, 2 * F), dout)
+    wp, wn = _gemm_ws(M, F, H, ws, split, dout.device)
+    _call("enc_glu_down_bwd_data", M, F, H, act, _ptr(dout), _ptr(w_2), _ptr(gu), _ptr(dgu), wp, wn, _stream(stream))
+    return dgu
+
+
+def enc_glu_up_bwd_data(dgu, w_gu, dy2=None, ws=None, split=True, stream=None):
+    M, F2 = dgu.shape
+    H = w_gu.shape[1]
+    if F2 % 2:
+        raise ValueError("dgu columns must be 2*F")
+    _check(dgu, "dgu", (M, F2))
+    _check(w_gu, "w_gu", (F2, H))
+    dy2 = _out(dy2, "dy2", (M, H), dgu)
+    wp, wn = _gemm_ws(M, H, F2, ws, split, dgu.device)
+    _call("enc_glu_up_bwd_data", M, H, F2 // 2, _ptr(dgu), _ptr(w_gu), _ptr(dy2), wp, wn, _stream(stream))
+    return dy2
+
+
+def enc_glu_up_bwd_weight(dgu, y2, dw_gu, db_gu=None, accumulate=False, ws=None, split=True, stream=None):
+    M, F2 = dgu.shape
+    H = y2.shape[1]
+    if F2 % 2:
+        raise ValueError("dgu columns must be 2*F")
+    _check(dgu, "dgu", (M, F2)); _check(y2, "y2", (M, H))
+    _check(dw_gu, "dw_gu", (F2, H), torch.float32)
+    if db_gu is not None:
+        _check(db_gu, "db_gu", (F2,), torch.float32)
+    return _named_wgrad("enc_glu_up_bwd_weight", M, H, F2 // 2, F2, H, dgu, y2, dw_gu, db_gu, accumulate, ws, split,
+                        stream)
 
 
 # ---------------------------------------------------------------- whole encoder

@@ -79,6 +79,10 @@ int check_mult8(const char *fn, std::initializer_list<int> dims) {
 // but tile indices and row counts are 32-bit).
 constexpr long kMaxElems = 1L << 31;
 
+// Packed sequences: the work list compares every pair of them, and a head
+// count and a sequence count this size keep every grid below 2^32 threads.
+constexpr int kMaxSeqs = 65536, kMaxHeads = 65536;
+
 // A launcher refused a shape that the argument checks accepted.  The checks
 // cover every refusal condition (check_cfg), so this is unreachable; if it
 // ever happens, kernels of the same call may already be enqueued, which is
@@ -294,6 +298,26 @@ bool gemm_wgrad(int M, int N, int K, const bf16_t *dY, const bf16_t *X, float *d
   return launch_gemm_wgrad(a, ws, ws_bytes, s, defer);
 }
 
+// [g | u][M, 2F] = Y[M, H] Wgu[2F, H]^T + b; h[M, F] = act(g) u
+bool glu_fwd(int M, int F, int H, int act, const bf16_t *Y, const bf16_t *W, const bf16_t *b, bf16_t *gu, bf16_t *h,
+             void *ws, size_t ws_bytes, hipStream_t s) {
+  GemmArgs a{};
+  a.M = M, a.N = 2 * F, a.K = H;
+  a.A = Y, a.lda = H, a.B = W, a.ldb = H;
+  a.Y = gu, a.ldy = 2 * F, a.bias = b, a.Y2 = h, a.act = act;
+  return launch_gemm_fwd(a, Epi::kGlu, ws, ws_bytes, s);
+}
+
+// dgu[M, 2F] from dh = dout[M, H] W2[H, F] and the saved [g | u]
+bool glu_dgrad(int M, int F, int H, int act, const bf16_t *dout, const bf16_t *W, const bf16_t *gu, bf16_t *dgu,
+               void *ws, size_t ws_bytes, hipStream_t s) {
+  GemmArgs a{};
+  a.M = M, a.N = F, a.K = H;
+  a.A = dout, a.lda = H, a.B = W, a.ldb = F;
+  a.Y = dgu, a.ldy = 2 * F, a.R = gu, a.act = act;
+  return launch_gemm_dgrad(a, Epi::kGluGrad, ws, ws_bytes, s);
+}
+
 int linear_dims(const char *fn, int M, std::initializer_list<int> feats) {
   int r = check_dims(fn, {M});
   if (r) return r;
@@ -402,6 +426,43 @@ int check_pgrads(const char *fn, const enc_pgrads_t *g) {
   c.req(g->kn_g, "dkn_g").req(g->kn_b, "dkn_b").req(g->w_o, "dw_o").req(g->b_o, "db_o");
   c.req(g->w_1, "dw_1").req(g->b_1, "db_1").req(g->w_2, "dw_2").req(g->b_2, "db_2");
   return c.code;
+}
+
+// Width of a packed qkv row and the limits of the kernels that read one.
+int packed_dims(const char *fn, int tokens, int heads, int kv_heads, int d) {
+  int r = check_dims(fn, {tokens, heads, kv_heads, d});
+  if (r) return r;
+  if (d != 64 && d != 80 && d != 128) return fail(ENC_ERR_UNSUPPORTED, "%s: head_dim must be 64, 80 or 128", fn);
+  if (heads % kv_heads) return fail(ENC_ERR_UNSUPPORTED, "%s: heads must be a multiple of kv_heads", fn);
+  if (heads > kMaxHeads || (static_cast<long>(heads) + 2L * kv_heads) * d * tokens >= kMaxElems)
+    return fail(ENC_ERR_UNSUPPORTED, "%s: tensor exceeds 2^31 elements, or heads exceed %d", fn, kMaxHeads);
+  return ENC_OK;
+}
+
+int packed_seqs(const char *fn, int tokens, int seqs) {
+  int r = check_dims(fn, {tokens, seqs});
+  if (r) return r;
+  if (seqs > kMaxSeqs) return fail(ENC_ERR_UNSUPPORTED, "%s: more than %d sequences", fn, kMaxSeqs);
+  return ENC_OK;
+}
+
+int attn_packed_dims(const char *fn, int tokens, int seqs, int heads, int kv_heads, int d, int causal) {
+  int r = packed_dims(fn, tokens, heads, kv_heads, d);
+  if (r || (r = packed_seqs(fn, tokens, seqs))) return r;
+  if (causal != 0 && causal != 1) return fail(ENC_ERR_INVALID, "%s: causal must be 0 or 1", fn);
+  // workgroups of 256 threads, two per item in the dK/dV kernel: fewer than 2^32 threads
+  if (static_cast<long>(packed_slots(tokens, seqs)) * heads >= 1L << 23)
+    return fail(ENC_ERR_UNSUPPORTED, "%s: (tokens / 128 + seqs) * heads must be below 2^23", fn);
+  return ENC_OK;
+}
+
+int glu_dims(const char *fn, int M, int H, int F, int act) {
+  if (F > (1 << 30)) return fail(ENC_ERR_UNSUPPORTED, "%s: tensor exceeds 2^31 elements", fn);
+  int r = linear_dims(fn, M, {H, F, 2 * F});
+  if (r) return r;
+  if (static_cast<long>(H) * 2 * F >= kMaxElems) return fail(ENC_ERR_UNSUPPORTED, "%s: weight exceeds 2^31 elements", fn);
+  if (act != ENC_GLU_SILU && act != ENC_GLU_GELU) return fail(ENC_ERR_INVALID, "%s: unknown activation %d", fn, act);
+  return ENC_OK;
 }
 
 int patch_dims(const char *fn, int B, int C, int ih, int iw, int p, int H, int has_cls, int *N, int *S, int *Kp) {
@@ -933,6 +994,162 @@ int enc_qk_norm_bwd(int M, int heads, int head_dim, const enc_bf16 *dqkvn, const
   launch_qk_norm_bwd(M, heads, head_dim, dqkvn, qkv, stats, qn_g, kn_g, dqkv, dqn_g, dqn_b, dkn_g, dkn_b,
                      accumulate ? 1 : 0, static_cast<float *>(ws), as_stream(stream));
   return launched(fn);
+}
+
+// ------------------------------------------------------------ packed sequences
+
+static int rope(const char *fn, int back, int M, int heads, int kv_heads, int head_dim, int sec_t, int sec_h,
+                int sec_w, int interleaved, const enc_bf16 *x, const int32_t *pos, const float *inv_freq, enc_bf16 *y,
+                enc_stream_t stream) {
+  int r = packed_dims(fn, M, heads, kv_heads, head_dim);
+  if (r) return r;
+  const long half = head_dim / 2;
+  if (sec_t < 0 || sec_h < 0 || sec_w < 0 || static_cast<long>(sec_t) + sec_h + sec_w > half)
+    return fail(ENC_ERR_INVALID, "%s: sections must not be negative nor sum to more than head_dim / 2", fn);
+  if (interleaved != 0 && interleaved != 1) return fail(ENC_ERR_INVALID, "%s: interleaved must be 0 or 1", fn);
+  PtrCheck c(fn);
+  c.req(x, back ? "dqkvr" : "qkv").req(pos, "pos").req(inv_freq, "inv_freq").req(y, back ? "dqkv" : "qkvr");
+  if (c.code) return c.code;
+  RopeArgs a{};
+  a.M = M, a.heads = heads, a.kv_heads = kv_heads, a.d = head_dim;
+  a.sec[0] = sec_t, a.sec[1] = sec_h, a.sec[2] = sec_w, a.interleaved = interleaved;
+  a.x = x, a.pos = pos, a.inv_freq = inv_freq, a.back = back, a.y = y;
+  if (!launch_rope(a, as_stream(stream))) return refused_after_checks(fn);
+  return launched(fn);
+}
+
+int enc_rope_fwd(int M, int heads, int kv_heads, int head_dim, int sec_t, int sec_h, int sec_w, int interleaved,
+                 const enc_bf16 *qkv, const int32_t *pos, const float *inv_freq, enc_bf16 *qkvr, enc_stream_t stream) {
+  return rope("enc_rope_fwd", 0, M, heads, kv_heads, head_dim, sec_t, sec_h, sec_w, interleaved, qkv, pos, inv_freq,
+              qkvr, stream);
+}
+
+int enc_rope_bwd(int M, int heads, int kv_heads, int head_dim, int sec_t, int sec_h, int sec_w, int interleaved,
+                 const enc_bf16 *dqkvr, const int32_t *pos, const float *inv_freq, enc_bf16 *dqkv,
+                 enc_stream_t stream) {
+  return rope("enc_rope_bwd", 1, M, heads, kv_heads, head_dim, sec_t, sec_h, sec_w, interleaved, dqkvr, pos, inv_freq,
+              dqkv, stream);
+}
+
+int enc_packed_plan_bytes(int tokens, int seqs, size_t *bytes) {
+  const char *fn = "enc_packed_plan_bytes";
+  int r = packed_seqs(fn, tokens, seqs);
+  if (r) return r;
+  if (!bytes) return fail(ENC_ERR_INVALID, "%s: bytes is NULL", fn);
+  *bytes = packed_plan_bytes(tokens, seqs);
+  return ok();
+}
+
+int enc_packed_plan(int tokens, int seqs, const int32_t *cu_seqlens, void *plan, size_t plan_bytes,
+                    enc_stream_t stream) {
+  const char *fn = "enc_packed_plan";
+  int r = packed_seqs(fn, tokens, seqs);
+  if (r) return r;
+  PtrCheck c(fn);
+  c.req(cu_seqlens, "cu_seqlens").req(plan, "plan");
+  if (c.code) return c.code;
+  const size_t need = packed_plan_bytes(tokens, seqs);
+  if (plan_bytes < need) return fail(ENC_ERR_WORKSPACE, "%s: plan %zu bytes < %zu needed", fn, plan_bytes, need);
+  if (!launch_packed_plan(tokens, seqs, cu_seqlens, static_cast<PackedPlan *>(plan), as_stream(stream)))
+    return refused_after_checks(fn);
+  return launched(fn);
+}
+
+int enc_attn_packed_fwd(int tokens, int seqs, int heads, int kv_heads, int head_dim, int causal, const void *plan,
+                        size_t plan_bytes, const enc_bf16 *qkv, enc_bf16 *o, float *lse, enc_stream_t stream) {
+  const char *fn = "enc_attn_packed_fwd";
+  int r = attn_packed_dims(fn, tokens, seqs, heads, kv_heads, head_dim, causal);
+  if (r) return r;
+  PtrCheck c(fn);
+  c.req(plan, "plan").req(qkv, "qkv").req(o, "o").req(lse, "lse");
+  if (c.code) return c.code;
+  const size_t need = packed_plan_bytes(tokens, seqs);
+  if (plan_bytes < need) return fail(ENC_ERR_WORKSPACE, "%s: plan %zu bytes < %zu needed", fn, plan_bytes, need);
+  PackedAttnArgs a{};
+  a.tokens = tokens, a.slots = packed_slots(tokens, seqs), a.heads = heads, a.kv_heads = kv_heads, a.d = head_dim;
+  a.causal = causal, a.plan = static_cast<const PackedPlan *>(plan), a.qkv = qkv, a.o = o, a.lse = lse;
+  if (!launch_attn_packed_fwd(a, as_stream(stream))) return refused_after_checks(fn);
+  return launched(fn);
+}
+
+int enc_attn_packed_bwd_workspace_bytes(int tokens, int heads, size_t *bytes) {
+  const char *fn = "enc_attn_packed_bwd_workspace_bytes";
+  int r = check_dims(fn, {tokens, heads});
+  if (r) return r;
+  if (static_cast<long>(tokens) * heads >= kMaxElems) return fail(ENC_ERR_UNSUPPORTED, "%s: tensor exceeds 2^31 elements", fn);
+  if (!bytes) return fail(ENC_ERR_INVALID, "%s: bytes is NULL", fn);
+  *bytes = attn_packed_bwd_ws_bytes(tokens, heads);
+  return ok();
+}
+
+int enc_attn_packed_bwd(int tokens, int seqs, int heads, int kv_heads, int head_dim, int causal, const void *plan,
+                        size_t plan_bytes, const enc_bf16 *qkv, const enc_bf16 *o, const float *lse,
+                        const enc_bf16 *do_, enc_bf16 *dqkv, void *ws, size_t ws_bytes, enc_stream_t stream) {
+  const char *fn = "enc_attn_packed_bwd";
+  int r = attn_packed_dims(fn, tokens, seqs, heads, kv_heads, head_dim, causal);
+  if (r) return r;
+  PtrCheck c(fn);
+  c.req(plan, "plan").req(qkv, "qkv").req(o, "o").req(lse, "lse").req(do_, "do").req(dqkv, "dqkv").req(ws, "ws");
+  if (c.code) return c.code;
+  const size_t pneed = packed_plan_bytes(tokens, seqs), need = attn_packed_bwd_ws_bytes(tokens, heads);
+  if (plan_bytes < pneed) return fail(ENC_ERR_WORKSPACE, "%s: plan %zu bytes < %zu needed", fn, plan_bytes, pneed);
+  if (ws_bytes < need) return fail(ENC_ERR_WORKSPACE, "%s: workspace %zu bytes < %zu needed", fn, ws_bytes, need);
+  PackedAttnArgs a{};
+  a.tokens = tokens, a.slots = packed_slots(tokens, seqs), a.heads = heads, a.kv_heads = kv_heads, a.d = head_dim;
+  a.causal = causal, a.plan = static_cast<const PackedPlan *>(plan), a.qkv = qkv;
+  a.o = const_cast<enc_bf16 *>(o), a.lse = const_cast<float *>(lse);  // read only in the backward
+  a.dO = do_, a.dqkv = dqkv, a.dvec = static_cast<float *>(ws);
+  if (!launch_attn_packed_bwd(a, as_stream(stream))) return refused_after_checks(fn);
+  return launched(fn);
+}
+
+// ------------------------------------------------------------ gated feed-forward
+
+int enc_glu_up_fwd(int M, int H, int F, int act, const enc_bf16 *y2, const enc_bf16 *w_gu, const enc_bf16 *b_gu,
+                   enc_bf16 *gu, enc_bf16 *h, void *ws, size_t ws_bytes, enc_stream_t stream) {
+  const char *fn = "enc_glu_up_fwd";
+  int r = glu_dims(fn, M, H, F, act);
+  if (r) return r;
+  PtrCheck c(fn);
+  c.req(y2, "y2").req(w_gu, "w_gu").opt(b_gu, "b_gu").opt(gu, "gu").req(h, "h");
+  if (c.code) return c.code;
+  if ((r = check_gemm_ws(fn, ws, ws_bytes, M, 2 * F, H))) return r;
+  if (!glu_fwd(M, F, H, act, y2, w_gu, b_gu, gu, h, ws, ws_bytes, as_stream(stream))) return refused_after_checks(fn);
+  return launched(fn);
+}
+
+int enc_glu_down_bwd_data(int M, int F, int H, int act, const enc_bf16 *dout, const enc_bf16 *w_2, const enc_bf16 *gu,
+                          enc_bf16 *dgu, void *ws, size_t ws_bytes, enc_stream_t stream) {
+  const char *fn = "enc_glu_down_bwd_data";
+  int r = glu_dims(fn, M, H, F, act);
+  if (r) return r;
+  PtrCheck c(fn);
+  c.req(dout, "dout").req(w_2, "w_2").req(gu, "gu").req(dgu, "dgu");
+  if (c.code) return c.code;
+  if ((r = check_gemm_ws(fn, ws, ws_bytes, M, F, H))) return r;
+  if (!glu_dgrad(M, F, H, act, dout, w_2, gu, dgu, ws, ws_bytes, as_stream(stream))) return refused_after_checks(fn);
+  return launched(fn);
+}
+
+int enc_glu_up_bwd_data(int M, int H, int F, const enc_bf16 *dgu, const enc_bf16 *w_gu, enc_bf16 *dy2, void *ws,
+                        size_t ws_bytes, enc_stream_t stream) {
+  const char *fn = "enc_glu_up_bwd_data";
+  int r = glu_dims(fn, M, H, F, ENC_GLU_SILU);
+  if (r) return r;
+  PtrCheck c(fn);
+  c.req(dgu, "dgu").req(w_gu, "w_gu").req(dy2, "dy2");
+  if (c.code) return c.code;
+  if ((r = check_gemm_ws(fn, ws, ws_bytes, M, H, 2 * F))) return r;
+  if (!gemm_dgrad(M, 2 * F, H, dgu, w_gu, nullptr, dy2, ws, ws_bytes, as_stream(stream)))
+    return refused_after_checks(fn);
+  return launched(fn);
+}
+
+int enc_glu_up_bwd_weight(int M, int H, int F, const enc_bf16 *dgu, const enc_bf16 *y2, float *dw_gu, float *db_gu,
+                          int accumulate, void *ws, size_t ws_bytes, enc_stream_t stream) {
+  int r = glu_dims("enc_glu_up_bwd_weight", M, H, F, ENC_GLU_SILU);
+  if (r) return r;
+  return enc_linear_bwd_weight(M, 2 * F, H, dgu, y2, dw_gu, db_gu, accumulate, ws, ws_bytes, stream);
 }
 
 int enc_parallel_saved_layout(const enc_cfg_t *cfg, enc_psaved_layout_t *layout) {

@@ -70,6 +70,62 @@ __device__ __forceinline__ float gelu_grad_f(float u) {
   return fmaf(u * 0.39894228040143268f, ex2, u >= 0.0f ? 1.0f - h : h);
 }
 
+// The gate's activation of a gated feed-forward block, and with its derivative:
+// SiLU(g) = g s, SiLU'(g) = s (1 + g (1 - s)), s = 1 / (1 + e^-g), or GELU.
+__device__ __forceinline__ float sigmoid_f(float g) {
+  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.4426950408889634f));
+}
+
+__device__ __forceinline__ float gate_f(float g, int act) {
+  if (act) return gelu_f(g);
+  return g * sigmoid_f(g);
+}
+
+__device__ __forceinline__ float gate_grad_f(float g, int act, float &value) {
+  if (act) {
+    float ex2;
+    const float h = phi_tail(g, ex2), phi = g >= 0.0f ? 1.0f - h : h;
+    value = g * phi;
+    return fmaf(g * 0.39894228040143268f, ex2, phi);
+  }
+  const float s = sigmoid_f(g);
+  value = g * s;
+  return s * fmaf(g, 1.0f - s, 1.0f);
+}
+
+// Eight outputs of a gated block, gate g and up-projection u in fp32:
+// h = act(g) u, and [g | u] themselves where they are kept.
+__device__ __forceinline__ void glu_store8(const float (&g)[8], const float (&u)[8], int act, bf16_t *gu_g,
+                                           bf16_t *gu_u, bf16_t *h) {
+  u32x4_t o;
+  if (gu_g) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = pack2(g[2 * e], g[2 * e + 1]);
+    stg16_nt(gu_g, o);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = pack2(u[2 * e], u[2 * e + 1]);
+    stg16_nt(gu_u, o);
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) o[e] = pack2(gate_f(g[2 * e], act) * u[2 * e], gate_f(g[2 * e + 1], act) * u[2 * e + 1]);
+  stg16_nt(h, o);
+}
+
+// Their gradients [dh u act'(g) | dh act(g)] from the saved g and u.
+__device__ __forceinline__ void glu_grad_store8(const float (&dh)[8], u32x4_t gw, u32x4_t uw, int act, bf16_t *dg,
+                                                bf16_t *du) {
+  u32x4_t o, w;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    float v0, v1;
+    const float d0 = gate_grad_f(lo_bf(gw[e]), act, v0), d1 = gate_grad_f(hi_bf(gw[e]), act, v1);
+    o[e] = pack2(dh[2 * e] * lo_bf(uw[e]) * d0, dh[2 * e + 1] * hi_bf(uw[e]) * d1);
+    w[e] = pack2(dh[2 * e] * v0, dh[2 * e + 1] * v1);
+  }
+  stg16_nt(dg, o);
+  stg16_nt(du, w);
+}
+
 // Logical tile for this workgroup.  MI355X dispatches workgroup i to XCD
 // i % 8.  When the tile grid splits evenly, the XCDs form two halves along M,
 // the four XCDs of a half split its column tiles, and each XCD walks its block
@@ -156,6 +212,34 @@ __device__ __forceinline__ void store_tile(const GemmArgs &p, const f32x16_t (&a
   for (int i = 0; i < FM; ++i) {
     const int m = m0 + wm * WTM + i * 32 + lrow;
     if (m >= p.M) continue;
+    if constexpr (EPI == Epi::kGlu) {
+      // fragment 0 holds gates, fragment 1 the same columns of the up-projection
+      static_assert(FN == 2, "a wave holds one gate and one up fragment");
+      const int F = p.N / 2;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int nb = n0 / 2 + wn * 32 + q * 8 + (lane >> 5) * 4;
+        if (nb >= F) continue;
+        const u32x2_t z{0u, 0u};
+        const u32x2_t bg = p.bias ? *reinterpret_cast<const u32x2_t *>(p.bias + nb) : z;
+        const u32x2_t bu = p.bias ? *reinterpret_cast<const u32x2_t *>(p.bias + F + nb) : z;
+        float g[4], u[4], h[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          g[e] = acc[i][0][q * 4 + e] + ((e & 1) ? hi_bf(bg[e >> 1]) : lo_bf(bg[e >> 1]));
+          u[e] = acc[i][1][q * 4 + e] + ((e & 1) ? hi_bf(bu[e >> 1]) : lo_bf(bu[e >> 1]));
+          h[e] = gate_f(g[e], p.act) * u[e];
+        }
+        if (p.Y) {
+          bf16_t *gu = p.Y + static_cast<size_t>(m) * p.N + nb;
+          *reinterpret_cast<u32x2_t *>(gu) = u32x2_t{pack2(g[0], g[1]), pack2(g[2], g[3])};
+          *reinterpret_cast<u32x2_t *>(gu + F) = u32x2_t{pack2(u[0], u[1]), pack2(u[2], u[3])};
+        }
+        *reinterpret_cast<u32x2_t *>(p.Y2 + static_cast<size_t>(m) * F + nb) =
+            u32x2_t{pack2(h[0], h[1]), pack2(h[2], h[3])};
+      }
+      continue;
+    }
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
 #pragma unroll
@@ -170,6 +254,20 @@ __device__ __forceinline__ void store_tile(const GemmArgs &p, const f32x16_t (&a
           f32x4_t w{v[0], v[1], v[2], v[3]};
           if (p.accumulate) w += *reinterpret_cast<const f32x4_t *>(p.Wf + off);
           *reinterpret_cast<f32x4_t *>(p.Wf + off) = w;
+        } else if constexpr (EPI == Epi::kGluGrad) {
+          const u32x2_t gw = *reinterpret_cast<const u32x2_t *>(p.R + off);
+          const u32x2_t uw = *reinterpret_cast<const u32x2_t *>(p.R + off + p.N);
+          float dg[4], du[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float gv = (e & 1) ? hi_bf(gw[e >> 1]) : lo_bf(gw[e >> 1]);
+            const float uv = (e & 1) ? hi_bf(uw[e >> 1]) : lo_bf(uw[e >> 1]);
+            float val;
+            dg[e] = v[e] * uv * gate_grad_f(gv, p.act, val);
+            du[e] = v[e] * val;
+          }
+          *reinterpret_cast<u32x2_t *>(p.Y + off) = u32x2_t{pack2(dg[0], dg[1]), pack2(dg[2], dg[3])};
+          *reinterpret_cast<u32x2_t *>(p.Y + off + p.N) = u32x2_t{pack2(du[0], du[1]), pack2(du[2], du[3])};
         } else {
           if constexpr (EPI == Epi::kBias || EPI == Epi::kBiasResid || EPI == Epi::kBiasGelu) {
             const u32x2_t bw = *reinterpret_cast<const u32x2_t *>(p.bias + nb);
@@ -225,7 +323,8 @@ __device__ __forceinline__ void store_tile_lds(const GemmArgs &p, const f32x4_t 
   constexpr int LDR = BN + 4;  // floats per LDS row (16-byte pad)
   constexpr int NCH = BM / kEpiRows;
   static_assert(BM % kEpiRows == 0 && kEpiRows % 16 == 0, "epilogue chunking");
-  constexpr bool kHasBias = EPI == Epi::kBias || EPI == Epi::kBiasResid || EPI == Epi::kBiasGelu;
+  constexpr bool kHasBias =
+      EPI == Epi::kBias || EPI == Epi::kBiasResid || EPI == Epi::kBiasGelu || EPI == Epi::kGlu;
   // a second per-element input: the residual, or the saved pre-activation u
   constexpr bool kHasR = EPI == Epi::kBiasResid || EPI == Epi::kResid || EPI == Epi::kGeluGrad;
   constexpr int PRB = BN / 8;                        // 16-byte bf16 segments per row
@@ -241,8 +340,15 @@ __device__ __forceinline__ void store_tile_lds(const GemmArgs &p, const f32x4_t 
   if constexpr (kHasBias) {
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
-      const int nb = n0 + wn * WTN + j * 16 + lcol;
-      bias_w[j] = nb < p.N ? *reinterpret_cast<const u32x2_t *>(p.bias + nb) : u32x2_t{0u, 0u};
+      if constexpr (EPI == Epi::kGlu) {
+        // the tile's first half of columns are gates, the second the same columns of the up-projection
+        const int v = wn * WTN + j * 16 + lcol, F = p.N / 2, c = n0 / 2 + (v < BN / 2 ? v : v - BN / 2);
+        const bool in = p.bias && c < F;
+        bias_w[j] = in ? *reinterpret_cast<const u32x2_t *>(p.bias + (v < BN / 2 ? c : F + c)) : u32x2_t{0u, 0u};
+      } else {
+        const int nb = n0 + wn * WTN + j * 16 + lcol;
+        bias_w[j] = nb < p.N ? *reinterpret_cast<const u32x2_t *>(p.bias + nb) : u32x2_t{0u, 0u};
+      }
     }
   }
   u32x4_t rin[kHasR ? NCH : 1][kHasR ? SEGS : 1];
@@ -258,8 +364,28 @@ __device__ __forceinline__ void store_tile_lds(const GemmArgs &p, const f32x4_t 
       }
   }
 
+  // the saved gate and up-projection of a gated block: two chunks' worth in
+  // registers, each chunk's loads issued before the stores of the one before
+  constexpr bool kGg = EPI == Epi::kGluGrad;
+  u32x4_t gin[kGg ? 2 : 1][kGg ? SEGS : 1], uin[kGg ? 2 : 1][kGg ? SEGS : 1];
+  auto load_gu = [&](int c) {
+    if constexpr (kGg) {
+#pragma unroll
+      for (int sg = 0; sg < SEGS; ++sg) {
+        const int it = tid + NT * sg;
+        const int gm = m0 + c * kEpiRows + it / PRB, gn = n0 + (it % PRB) * 8;
+        const bool in = it < kEpiRows * PRB && gm < p.M && gn < p.N;
+        const size_t off = static_cast<size_t>(gm) * p.ldy + gn;
+        gin[c & 1][sg] = in ? ldg16(p.R + off) : u32x4_t{0u, 0u, 0u, 0u};
+        uin[c & 1][sg] = in ? ldg16(p.R + off + p.N) : u32x4_t{0u, 0u, 0u, 0u};
+      }
+    }
+  };
+  load_gu(0);
+
 #pragma unroll
   for (int c = 0; c < NCH; ++c) {
+    if (c + 1 < NCH) load_gu(c + 1);
     __syncthreads();  // LDS free (k-loop reads or the previous chunk's readers done)
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
@@ -290,6 +416,22 @@ __device__ __forceinline__ void store_tile_lds(const GemmArgs &p, const f32x4_t 
         if (p.accumulate) v += *reinterpret_cast<const f32x4_t *>(p.Wf + off);
         stg16_nt(p.Wf + off, v);
       }
+    } else if constexpr (EPI == Epi::kGlu) {
+      constexpr int PRH = BN / 16;  // 16-byte segments of a row's gates
+      const int F = p.N / 2;
+      for (int it = tid; it < kEpiRows * PRH; it += NT) {
+        const int r = it / PRH, cc = (it % PRH) * 8;
+        const int gm = m0 + c * kEpiRows + r, gn = n0 / 2 + cc;
+        if (gm >= p.M || gn >= F) continue;
+        float g[8], u[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          g[e] = lds[r * LDR + cc + e];
+          u[e] = lds[r * LDR + BN / 2 + cc + e];
+        }
+        bf16_t *gu = p.Y ? p.Y + static_cast<size_t>(gm) * p.N + gn : nullptr;
+        glu_store8(g, u, p.act, gu, gu + F, p.Y2 + static_cast<size_t>(gm) * F + gn);
+      }
     } else {
 #pragma unroll
       for (int sg = 0; sg < SEGS; ++sg) {
@@ -301,6 +443,10 @@ __device__ __forceinline__ void store_tile_lds(const GemmArgs &p, const f32x4_t 
         const f32x4_t b = *reinterpret_cast<const f32x4_t *>(lds + r * LDR + cc + 4);
         float v[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
         const size_t off = static_cast<size_t>(gm) * p.ldy + gn;
+        if constexpr (kGg) {
+          glu_grad_store8(v, gin[c & 1][sg], uin[c & 1][sg], p.act, p.Y + off, p.Y + off + p.N);
+          continue;
+        }
         if constexpr (EPI == Epi::kBiasResid || EPI == Epi::kResid) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
@@ -341,13 +487,21 @@ struct TileLoader<ROWS, BK, NT, false> {
   static_assert(ROWS * KC % NT == 0, "tile chunks must divide the threads");
   u32x4_t r[CH];
 
+  // GLU: rows [F gates][F up-projections]; every 64 tile rows are 32 gates and
+  // the same 32 of the up-projection
+  template <bool GLU = false>
   __device__ __forceinline__ void load(const bf16_t *__restrict__ X, int ld, int rows, int K, int r0, int k0,
                                        int tid) {
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
       const int c = tid + NT * i;
       const int row = c / KC, kc = c % KC;
-      const int gr = r0 + row, gk = k0 + kc * 8;
+      int gr = r0 + row;
+      const int gk = k0 + kc * 8;
+      if constexpr (GLU) {
+        const int col = r0 / 2 + (row >> 6) * 32 + (row & 31);
+        gr = col >= rows / 2 ? rows : (row & 32) ? rows / 2 + col : col;
+      }
       if (gr < rows && gk < K)
         r[i] = ldg16(X + static_cast<size_t>(gr) * ld + gk);
       else
@@ -374,8 +528,10 @@ struct TileLoader<ROWS, BK, NT, true> {
   static constexpr int TB = (NBLK + NT - 1) / NT;
   u32x4_t r[TB][8];
 
+  template <bool GLU = false>
   __device__ __forceinline__ void load(const bf16_t *__restrict__ X, int ld, int rows, int K, int r0, int k0,
                                        int tid) {
+    static_assert(!GLU, "a gated block's weight is contraction-contiguous");
 #pragma unroll
     for (int t = 0; t < TB; ++t) {
       const int b = tid + NT * t;
@@ -454,7 +610,7 @@ __global__ __launch_bounds__(WM *WN * 64) void gemm_kernel(GemmArgs p) {
 
   const int nk = (p.K + BK - 1) / BK;
   la.load(p.A, p.lda, p.M, p.K, m0, 0, tid);
-  lb.load(p.B, p.ldb, p.N, p.K, n0, 0, tid);
+  lb.template load<EPI == Epi::kGlu>(p.B, p.ldb, p.N, p.K, n0, 0, tid);
   if constexpr (kDb) {
     if (do_db) la.rowsum(dbacc);
   }
@@ -469,7 +625,7 @@ __global__ __launch_bounds__(WM *WN * 64) void gemm_kernel(GemmArgs p) {
     const bool more = (t + 1) < nk;
     if (more) {
       la.load(p.A, p.lda, p.M, p.K, m0, (t + 1) * BK, tid);
-      lb.load(p.B, p.ldb, p.N, p.K, n0, (t + 1) * BK, tid);
+      lb.template load<EPI == Epi::kGlu>(p.B, p.ldb, p.N, p.K, n0, (t + 1) * BK, tid);
     }
 #pragma unroll
     for (int kk = 0; kk < BK / 16; ++kk) {
@@ -665,8 +821,11 @@ struct HalfTile {
   u32x4_t rsrc;
   int off[NOFF];  // LDS offset of this wave's fragments in a half tile
 
+  // GLU: the second half of the tile's rows lie `skip` rows further on
+  template <bool GLU = false>
   __device__ __forceinline__ void init(const bf16_t *base, uint32_t nbytes, int ld, int r0, int w, int wid, int lane,
-                                       int lds_base) {
+                                       int lds_base, int skip = 0) {
+    static_assert(!GLU || (!TRANS && NWV % 2 == 0), "a wave's rows lie in one half");
     rsrc = make_rsrc(base, nbytes);
     half_off = __builtin_amdgcn_readfirstlane(TRANS ? HR * 2 : static_cast<uint32_t>(HR) * ld * 2);
 #pragma unroll
@@ -677,7 +836,8 @@ struct HalfTile {
         using T = NtTile<BK>;
         const int br = o / T::RB, pch = (o % T::RB) >> 4;
         const int c = pch ^ ((br / T::RP) % T::CPR);
-        const int r = br / HR * WROWS + br % HR;
+        int r = br / HR * WROWS + br % HR;
+        if constexpr (GLU) r += r >= ROWS ? skip : 0;
         voff[i] = static_cast<uint32_t>(((r0 + r) * static_cast<long>(ld) + c * 8) * 2);
       } else {
         const int k = o / (LROWS * 2), pch = (o % (LROWS * 2)) >> 4;
@@ -761,7 +921,10 @@ __global__ __launch_bounds__(512, 1) void gemm_half_kernel(GemmArgs p, uint32_t 
   TB lb;
   const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(smem));
   la.init(p.A, a_bytes, p.lda, m0, wm, wid, lane, 0);
-  lb.init(p.B, b_bytes, p.ldb, n0, wn, wid, lane, B_BASE);
+  if constexpr (EPI == Epi::kGlu)
+    lb.template init<true>(p.B, b_bytes, p.ldb, n0 / 2, wn, wid, lane, B_BASE, p.N / 2 - BN / 2);
+  else
+    lb.init(p.B, b_bytes, p.ldb, n0, wn, wid, lane, B_BASE);
   const uint32_t a_step = AT ? static_cast<uint32_t>(BK) * p.lda * 2 : BK * 2;
   const uint32_t b_step = BT ? static_cast<uint32_t>(BK) * p.ldb * 2 : BK * 2;
   // byte offsets of the k-step whose loads are issued next
@@ -1014,16 +1177,20 @@ struct RingTile {
   __device__ static __forceinline__ int swz(int k) {
     return ROWS % 128 == 0 ? t_swz(k) : ((((k >> 1) & 1) | (((k >> 3) & 1) << 1)) << 1);
   }
+  template <bool GLU = false>
   __device__ __forceinline__ void init(const bf16_t *base, uint32_t nbytes, int ld, int r0, int w, int wid, int lane,
-                                       int lds_base) {
+                                       int lds_base, int skip = 0) {
+    static_assert(!GLU || !TRANS, "a gated block's weight is contraction-contiguous");
     rsrc = make_rsrc(base, nbytes);
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
       const int o = wid * WB + i * 1024 + lane * 16;
       if constexpr (!TRANS) {
         using T = NtTile<BK>;
-        const int r = o / T::RB, pch = (o % T::RB) >> 4;
+        int r = o / T::RB;
+        const int pch = (o % T::RB) >> 4;
         const int c = pch ^ ((r / T::RP) % T::CPR);
+        if constexpr (GLU) r += r >= ROWS / 2 ? skip : 0;
         voff[i] = static_cast<uint32_t>(((r0 + r) * static_cast<long>(ld) + c * 8) * 2);
       } else {
         const int k = o / (ROWS * 2), pch = (o % (ROWS * 2)) >> 4;
@@ -1112,7 +1279,10 @@ __global__ __launch_bounds__(512, 2 * WGS) void gemm_ring_kernel(GemmArgs p, uin
   TB lb;
   const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(smem));
   la.init(p.A, a_bytes, p.lda, m0, wm, wid, lane, 0);
-  lb.init(p.B, b_bytes, p.ldb, n0, wn, wid, lane, B_BASE);
+  if constexpr (EPI == Epi::kGlu)
+    lb.template init<true>(p.B, b_bytes, p.ldb, n0 / 2, wn, wid, lane, B_BASE, p.N / 2 - BN / 2);
+  else
+    lb.init(p.B, b_bytes, p.ldb, n0, wn, wid, lane, B_BASE);
   const uint32_t a_step = AT ? static_cast<uint32_t>(BK) * p.lda * 2 : BK * 2;
   const uint32_t b_step = BT ? static_cast<uint32_t>(BK) * p.ldb * 2 : BK * 2;
   uint32_t so_a = AT ? static_cast<uint32_t>(kbeg) * p.lda * 2 : static_cast<uint32_t>(kbeg) * 2;
@@ -1255,6 +1425,12 @@ bool launch_ring_cfg(const GemmArgs &a, uint32_t a_bytes, uint32_t b_bytes, hipS
   return true;
 }
 
+// Whether an epilogue evaluates an activation (those products have rows of the
+// cost table of their own).
+constexpr bool has_activation(Epi e) {
+  return e == Epi::kBiasGelu || e == Epi::kGeluGrad || e == Epi::kGlu || e == Epi::kGluGrad;
+}
+
 // Direct-to-LDS path on tile t (of kTiles): 256-row tiles run gemm_half_kernel,
 // the others gemm_ring_kernel.
 // Returns false when the operands do not fit the path's constraints.  Only the
@@ -1262,7 +1438,7 @@ bool launch_ring_cfg(const GemmArgs &a, uint32_t a_bytes, uint32_t b_bytes, hipS
 // input-gradient products write fp32 as partials of a split only).
 template <bool AT, bool BT, Epi EPI>
 bool launch_lds(const GemmArgs &a, hipStream_t s, TileShape t) {
-  constexpr bool gelu = EPI == Epi::kBiasGelu || EPI == Epi::kGeluGrad;
+  constexpr bool gelu = has_activation(EPI);
   constexpr GemmLayout row = !AT && EPI == Epi::kF32 ? kSplit : gemm_layout(AT, BT, gelu);
   if (!lds_fits(a.M, a.N, a.K, a.lda, a.ldb, AT, BT)) return false;
   // operand extents (bytes) bound the buffer loads
@@ -1297,7 +1473,7 @@ bool launch_lds(const GemmArgs &a, hipStream_t s, TileShape t) {
 
 template <bool AT, bool BT, Epi EPI>
 bool launch_lds(const GemmArgs &a, hipStream_t s) {
-  constexpr bool gelu = EPI == Epi::kBiasGelu || EPI == Epi::kGeluGrad;
+  constexpr bool gelu = has_activation(EPI);
   return launch_lds<AT, BT, EPI>(a, s, choose_tile(a.M, a.N, a.K, gemm_layout(AT, BT, gelu)));
 }
 
@@ -1361,6 +1537,56 @@ __global__ __launch_bounds__(256) void splitk_epilogue_kernel(const float *__res
   }
 }
 
+// The same for a gated block.  kGlu: partials [S][M][2F]; writes h and, where
+// gu is given, [g | u].  kGluGrad: partials [S][M][F] of dh and the saved
+// [g | u] in R; writes its gradient to gu.  Eight columns of F per thread and
+// iteration.
+template <Epi EPI>
+__global__ __launch_bounds__(256) void splitk_glu_kernel(const float *__restrict__ part, int splits, size_t stride,
+                                                         int M, int F, int act, const bf16_t *__restrict__ bias,
+                                                         const bf16_t *__restrict__ R, bf16_t *__restrict__ gu,
+                                                         bf16_t *__restrict__ h) {
+  constexpr bool kFwd = EPI == Epi::kGlu;
+  const int per_row = F / 8;
+  const long n8 = static_cast<long>(M) * per_row;
+  auto sum8 = [&](size_t at, float (&v)[8]) {
+    f32x4_t lo = *reinterpret_cast<const f32x4_t *>(part + at), hi = *reinterpret_cast<const f32x4_t *>(part + at + 4);
+    for (int sp = 1; sp < splits; ++sp) {
+      lo += *reinterpret_cast<const f32x4_t *>(part + sp * stride + at);
+      hi += *reinterpret_cast<const f32x4_t *>(part + sp * stride + at + 4);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = lo[e], v[e + 4] = hi[e];
+  };
+  auto add_bias = [&](const bf16_t *b, float (&v)[8]) {
+    const u32x4_t w = ldg16(b);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[2 * e] += lo_bf(w[e]);
+      v[2 * e + 1] += hi_bf(w[e]);
+    }
+  };
+  for (long i = blockIdx.x * 256L + threadIdx.x; i < n8; i += static_cast<long>(gridDim.x) * 256) {
+    const size_t m = i / per_row;
+    const int c = static_cast<int>(i % per_row) * 8;
+    const size_t at2 = m * 2 * F + c;  // in the rows of 2F
+    if constexpr (kFwd) {
+      float g[8], u[8];
+      sum8(at2, g);
+      sum8(at2 + F, u);
+      if (bias) {
+        add_bias(bias + c, g);
+        add_bias(bias + F + c, u);
+      }
+      glu_store8(g, u, act, gu ? gu + at2 : nullptr, gu + at2 + F, h + m * F + c);
+    } else {
+      float dh[8];
+      sum8(m * F + c, dh);
+      glu_grad_store8(dh, ldg16(R + at2), ldg16(R + at2 + F), act, gu + at2, gu + at2 + F);
+    }
+  }
+}
+
 // Split launch of a forward (AT = false, BT = false) or input-gradient
 // (BT = true) product: fp32 partials into ws, then the epilogue kernel.
 // Returns false (nothing launched) when the plan does not split or ws is
@@ -1368,9 +1594,11 @@ __global__ __launch_bounds__(256) void splitk_epilogue_kernel(const float *__res
 template <bool BT, Epi EPI>
 bool launch_split(const GemmArgs &a, void *ws, size_t ws_bytes, hipStream_t s) {
   const SplitPlan sp = gemm_split_plan(a.M, a.N, a.K);
-  if (sp.splits <= 1 || ws == nullptr || ws_bytes < gemm_ws_bytes(a.M, a.N, a.K) || a.ldy != a.N || a.N % 8)
+  if (sp.splits <= 1 || ws == nullptr || ws_bytes < gemm_ws_bytes(a.M, a.N, a.K) ||
+      a.ldy != (EPI == Epi::kGluGrad ? 2 * a.N : a.N) || a.N % 8)
     return false;
   GemmArgs b = a;
+  b.ldy = a.N;
   b.splits = sp.splits;
   b.k_chunk = sp.k_chunk;
   b.split_stride = static_cast<size_t>(a.M) * a.N;
@@ -1378,10 +1606,17 @@ bool launch_split(const GemmArgs &a, void *ws, size_t ws_bytes, hipStream_t s) {
   b.db = nullptr;
   b.accumulate = 0;
   if (!launch_lds<false, BT, Epi::kF32>(b, s, sp.tile)) return false;
-  const long n8 = static_cast<long>(a.M) * a.N / 8;
-  const int blocks = static_cast<int>(std::min<long>((n8 + 255) / 256, 2048));
-  hipLaunchKernelGGL((splitk_epilogue_kernel<EPI>), dim3(blocks), dim3(256), 0, s, b.Wf, sp.splits, b.split_stride,
-                     a.M, a.N, a.bias, a.R, a.Y, a.Y2);
+  if constexpr (EPI == Epi::kGlu || EPI == Epi::kGluGrad) {
+    const int F = EPI == Epi::kGlu ? a.N / 2 : a.N;
+    const long f8 = static_cast<long>(a.M) * F / 8;
+    hipLaunchKernelGGL((splitk_glu_kernel<EPI>), dim3(static_cast<int>(std::min<long>((f8 + 255) / 256, 2048))),
+                       dim3(256), 0, s, b.Wf, sp.splits, b.split_stride, a.M, F, a.act, a.bias, a.R, a.Y, a.Y2);
+  } else {
+    const long n8 = static_cast<long>(a.M) * a.N / 8;
+    const int blocks = static_cast<int>(std::min<long>((n8 + 255) / 256, 2048));
+    hipLaunchKernelGGL((splitk_epilogue_kernel<EPI>), dim3(blocks), dim3(256), 0, s, b.Wf, sp.splits, b.split_stride,
+                       a.M, a.N, a.bias, a.R, a.Y, a.Y2);
+  }
   return true;
 }
 
@@ -1405,6 +1640,7 @@ bool launch_gemm_fwd(const GemmArgs &a, Epi epi, void *ws, size_t ws_bytes, hipS
     case Epi::kBiasResid: return fwd_any<Epi::kBiasResid>(a, ws, ws_bytes, s);
     case Epi::kBiasGelu: return fwd_any<Epi::kBiasGelu>(a, ws, ws_bytes, s);
     case Epi::kPlain: return fwd_any<Epi::kPlain>(a, ws, ws_bytes, s);
+    case Epi::kGlu: return fwd_any<Epi::kGlu>(a, ws, ws_bytes, s);
     default: return false;
   }
 }
@@ -1414,6 +1650,7 @@ bool launch_gemm_dgrad(const GemmArgs &a, Epi epi, void *ws, size_t ws_bytes, hi
     case Epi::kPlain: return dgrad_any<Epi::kPlain>(a, ws, ws_bytes, s);
     case Epi::kGeluGrad: return dgrad_any<Epi::kGeluGrad>(a, ws, ws_bytes, s);
     case Epi::kResid: return dgrad_any<Epi::kResid>(a, ws, ws_bytes, s);
+    case Epi::kGluGrad: return dgrad_any<Epi::kGluGrad>(a, ws, ws_bytes, s);
     default: return false;
   }
 }

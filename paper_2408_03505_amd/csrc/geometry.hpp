@@ -53,6 +53,34 @@ inline size_t attn_bwd_ws_bytes(int B, int S, int heads) {
   return static_cast<size_t>(B) * heads * S * sizeof(float);
 }
 
+// ---- Packed sequences: the work list that packed attention reads.  One item
+// per kPackedRows tokens of a sequence; a batch of `tokens` rows in `seqs`
+// sequences has at most packed_slots of them.
+constexpr int kPackedRows = 128;
+
+struct PackedItem {
+  int first, len;  // the sequence's first row and its tokens
+  int row;         // the item's first token in the sequence
+  int pad;
+};
+
+struct PackedPlan {
+  int count, pad[3];
+  PackedItem item[1];
+};
+
+inline int packed_slots(int tokens, int seqs) { return tokens / kPackedRows + seqs; }
+
+inline size_t packed_plan_bytes(int tokens, int seqs) {
+  const size_t b = sizeof(PackedItem) * (1 + static_cast<size_t>(tokens / kPackedRows) + seqs);
+  return (b + 255) & ~static_cast<size_t>(255);
+}
+
+// ---- Packed attention backward: the D vector, one fp32 per head and row.
+inline size_t attn_packed_bwd_ws_bytes(int tokens, int heads) {
+  return static_cast<size_t>(heads) * tokens * sizeof(float);
+}
+
 // ---- GEMM tile choice.  The direct-to-LDS kernels come in these output
 // tiles; per_cu workgroups of a tile share a CU.  cost[kind] is the time in us
 // of one workgroup per 64-wide k-step and on top of them (prologue, epilogue):

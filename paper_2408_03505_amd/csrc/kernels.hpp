@@ -51,6 +51,12 @@ enum class Epi : int {
   kPlain = 4,      // Y = acc                                 (bf16 out)
   kF32 = 5,        // Wf (+)= acc; optional fused db         (fp32 out)
   kResid = 6,      // Y = acc + R[m, n]                       (bf16 out)
+  // gated feed-forward, F = N / 2: [g | u] = acc + bias; Y = [g | u] (optional),
+  // Y2[m, F] = act(g) u                                      (bf16 outs)
+  kGlu = 7,
+  // its gradient through the down-projection, N = F: with [g | u] = R[m, 2F]
+  // and dh = acc, Y[m, 2F] = [dh u act'(g) | dh act(g)]      (bf16 out)
+  kGluGrad = 8,
 };
 
 struct GemmArgs {
@@ -67,6 +73,7 @@ struct GemmArgs {
   float *Wf;           // fp32 output [M, ldy]
   float *db;           // fused row sums of A over k (fp32, [M]) for the weight gradient
   int accumulate;
+  int act;  // gated feed-forward: the gate's activation (0 SiLU, 1 GELU)
   // Split contraction: when splits > 1, workgroup split s of a tile covers
   // k in [s * k_chunk, min(K, (s + 1) * k_chunk)) (k_chunk a multiple of the
   // k-step) and writes its fp32 partial to Wf + s * split_stride (and, for a
@@ -106,6 +113,35 @@ bool launch_attn_bwd(int B, int S, int heads, int d, const bf16_t *qkv, const bf
 // current device's address of the array (looked up once per device).
 constexpr size_t kAttnScratchFloats = static_cast<size_t>(1) << 20;
 hipError_t attn_bwd_scratch(float **ptr);
+
+// ---- Rotary positions (forward, or with `back` the rotation undone)
+struct RopeArgs {
+  int M, heads, kv_heads, d;
+  int sec[3];       // pairs of each axis
+  int interleaved;  // pairs (2i, 2i + 1), else (i, i + d / 2)
+  const bf16_t *x;  // [M, (heads + 2 kv_heads) d]
+  const int *pos;   // [M, 3]
+  const float *inv_freq;
+  int back;
+  bf16_t *y;  // may be x
+};
+bool launch_rope(const RopeArgs &a, hipStream_t s);
+
+// ---- Packed sequences
+bool launch_packed_plan(int tokens, int seqs, const int *cu, PackedPlan *plan, hipStream_t s);
+
+struct PackedAttnArgs {
+  int tokens, slots, heads, kv_heads, d, causal;
+  const PackedPlan *plan;
+  const bf16_t *qkv;  // [tokens, (heads + 2 kv_heads) d]
+  bf16_t *o;          // [tokens, heads d]
+  float *lse;         // [heads, tokens]
+  const bf16_t *dO;
+  bf16_t *dqkv;
+  float *dvec;  // [heads, tokens]
+};
+bool launch_attn_packed_fwd(const PackedAttnArgs &a, hipStream_t s);
+bool launch_attn_packed_bwd(const PackedAttnArgs &a, hipStream_t s);
 
 // ---- Patch embedding (images -> patch rows; tokens + class token + positions)
 bool launch_patchify(int B, int C, int img_h, int img_w, int p, int Kp, const bf16_t *images, bf16_t *patches,

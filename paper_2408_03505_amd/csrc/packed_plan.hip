@@ -1,0 +1,69 @@
+// Work list of a packed batch: its sequences cut into tiles of kPackedRows
+// tokens, the longest sequence first, so that an attention launch starts its
+// longest workgroups first and ends with short ones.  Built on the GPU from the
+// sequences' offsets, once per batch, and read by every attention launch on it.
+//
+// Bound by latency.  Every sequence counts the tiles that precede its own (of
+// sequences with more tiles, or as many and a lower index), so no sort, atomic
+// or second launch is needed and the list is the same every time; that is
+// seqs^2 comparisons, 256 sequences to a workgroup.
+#include "common.hpp"
+#include "kernels.hpp"
+
+namespace optimus {
+
+namespace {
+
+// First token and token count of sequence i, kept inside [0, tokens) whatever
+// the offsets hold.
+__device__ __forceinline__ void sequence(const int *cu, int i, int tokens, int &first, int &len) {
+  first = min(max(cu[i], 0), tokens);
+  len = min(max(cu[i + 1], first), tokens) - first;
+}
+
+__device__ __forceinline__ int tiles_of(int len) { return (len + kPackedRows - 1) / kPackedRows; }
+
+__global__ __launch_bounds__(256) void packed_plan_kernel(int tokens, int seqs, int cap, const int *__restrict__ cu,
+                                                          PackedPlan *__restrict__ plan) {
+  __shared__ int tiles[256], first_item[256], firsts[256], lens[256];
+  const int tid = threadIdx.x, mine = blockIdx.x * 256 + tid;
+  int first = 0, len = 0;
+  if (mine < seqs) sequence(cu, mine, tokens, first, len);
+  const int t = tiles_of(len);
+  long before = 0, total = 0;
+  for (int j0 = 0; j0 < seqs; j0 += 256) {
+    int f, l = 0;
+    if (j0 + tid < seqs) sequence(cu, j0 + tid, tokens, f, l);
+    __syncthreads();
+    tiles[tid] = tiles_of(l);
+    __syncthreads();
+    const int n = min(256, seqs - j0);
+    for (int j = 0; j < n; ++j) {
+      const int o = tiles[j];
+      total += o;
+      if (o > t || (o == t && j0 + j < mine)) before += o;
+    }
+  }
+  // (offsets that go backwards could ask for more items than there is room for)
+  first_item[tid] = static_cast<int>(min(before, static_cast<long>(cap)));
+  firsts[tid] = first;
+  lens[tid] = len;
+  __syncthreads();
+  for (int j = 0; j < min(256, seqs - static_cast<int>(blockIdx.x) * 256); ++j) {
+    const int nt = tiles_of(lens[j]);
+    for (int k = tid; k < nt && first_item[j] + k < cap; k += 256)
+      // the last tile first: with causal attention it is the longest
+      plan->item[first_item[j] + k] = PackedItem{firsts[j], lens[j], (nt - 1 - k) * kPackedRows, 0};
+  }
+  if (mine == 0) plan->count = static_cast<int>(min(total, static_cast<long>(cap)));
+}
+
+}  // namespace
+
+bool launch_packed_plan(int tokens, int seqs, const int *cu, PackedPlan *plan, hipStream_t s) {
+  hipLaunchKernelGGL(packed_plan_kernel, dim3((seqs + 255) / 256), dim3(256), 0, s, tokens, seqs,
+                     packed_slots(tokens, seqs), cu, plan);
+  return true;
+}
+
+}  // namespace optimus
