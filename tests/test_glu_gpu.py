@@ -1,0 +1,173 @@
+"""The gated feed-forward products on the GPU against the float64 oracle within
+its elementwise bounds: every tile that their launch plan gives them, whole and
+as splits of the contraction, and the kernel that stages through registers."""
+
+import numpy as np
+import pytest
+import torch
+
+from helpers import announce, cuda, f64, guard_intact, guarded
+from oracle import packed as P
+from paper_2408_03505_amd import binding as B
+from paper_2408_03505_amd.synthetic import random_bf16
+
+gpu = pytest.mark.gpu
+BF = torch.bfloat16
+ACTS = {"silu": B.GLU_SILU, "gelu": B.GLU_GELU}
+
+# (rows, F) smallest first; between them and these contractions every tile that
+# the products are offered runs, in every phase of its ring
+SIZES = sorted([(1, 8), (40, 72), (120, 200), (300, 520), (257, 1000), (200, 4224), (776, 1304), (1030, 2056),
+                (6570, 264), (6570, 528), (2050, 1032), (5400, 528), (980, 5544), (1500, 2056), (4100, 1032),
+                (7350, 528), (7610, 792), (1030, 5504), (2050, 4008), (7610, 1584)], key=lambda s: s[0] * s[1])
+STEPS = (1, 2, 3, 4, 5, 8, 20)
+
+
+def _cases(layout, steps):
+    """Per tile the smallest size that runs on it, unsplit, at this contraction."""
+    out = {}
+    for M, F in SIZES:
+        if M * F * steps > 2.5e8:  # (the oracle's time)
+            continue
+        bm, bn, sp = B.linear_plan(layout, M, 2 * F if layout == B.LAYOUT_FWD_GELU else F, 64 * steps)
+        if sp == 1:
+            out.setdefault((bm, bn), (M, F))
+    return sorted(out.items())
+
+
+@pytest.mark.parametrize("layout", [B.LAYOUT_FWD_GELU, B.LAYOUT_DGRAD_GELU])
+def test_the_sizes_reach_the_tiles(layout):
+    tiles = {t for s in STEPS for t, _ in _cases(layout, s)}
+    every = {(256, 256), (256, 192), (128, 192), (128, 128), (64, 192), (64, 128), (64, 64)}
+    every |= {(128, 256)} if layout == B.LAYOUT_FWD_GELU else {(192, 128)}
+    assert every <= tiles, every - tiles
+
+
+def _within(got, ref, bound, what):
+    g = f64(got)
+    assert np.isfinite(g).all(), what
+    off = np.abs(g - ref)
+    assert (off <= bound).all(), f"{what}: worst error is {(off / np.maximum(bound, 1e-300)).max():.2f} of its bound"
+
+
+def _forward(M, H, F, act, bias=True, save=True, split=True, seed=0):
+    announce(f"glu_up_fwd M={M} H={H} F={F} {act} bias={bias} save={save} split={split}")
+    y, w = random_bf16((M, H), seed), random_bf16((2 * F, H), seed + 1, 1.5 / H ** 0.5)
+    b = random_bf16((2 * F,), seed + 2) if bias else None
+    gu, gbuf = guarded((M, 2 * F), BF)
+    h, hbuf = guarded((M, F), BF)
+    B.enc_glu_up_fwd(cuda(y), cuda(w), cuda(b) if bias else None, act=ACTS[act], gu=gu if save else None, h=h, save=save,
+                     split=split)
+    torch.cuda.synchronize()
+    rgu, rh, gb, hb = P.glu_fwd(f64(y), f64(w), f64(b) if bias else None, act)
+    what = f"{M}x{H}x{F} {act}"
+    _within(h, rh, hb, what)
+    if save:
+        _within(gu, rgu, gb, what)
+    assert guard_intact(hbuf, h.numel()) and guard_intact(gbuf, gu.numel())
+
+
+def _backward(M, H, F, act, split=True, seed=10):
+    announce(f"glu_down_bwd_data M={M} H={H} F={F} {act} split={split}")
+    dout, w2, gu = random_bf16((M, H), seed), random_bf16((H, F), seed + 1, 1.0 / H ** 0.5), random_bf16((M, 2 * F), seed + 2, 2.0)
+    dgu, buf = guarded((M, 2 * F), BF)
+    B.enc_glu_down_bwd_data(cuda(dout), cuda(w2), cuda(gu), act=ACTS[act], dgu=dgu, split=split)
+    torch.cuda.synchronize()
+    ref, bound = P.glu_bwd(f64(dout), f64(w2), f64(gu), act)
+    _within(dgu, ref, bound, f"{M}x{H}x{F} {act}")
+    assert guard_intact(buf, dgu.numel())
+
+
+@gpu
+@pytest.mark.parametrize("steps", STEPS)
+def test_forward_tiles(steps):
+    for i, (_, (M, F)) in enumerate(_cases(B.LAYOUT_FWD_GELU, steps)):
+        _forward(M, 64 * steps, F, "gelu" if (i + steps) % 3 == 0 else "silu", bias=(i + steps) % 2 == 0, seed=100 * i)
+
+
+@gpu
+@pytest.mark.parametrize("steps", STEPS)
+def test_backward_tiles(steps):
+    for i, (_, (M, F)) in enumerate(_cases(B.LAYOUT_DGRAD_GELU, steps)):
+        _backward(M, 64 * steps, F, "gelu" if (i + steps) % 3 == 0 else "silu", seed=100 * i)
+
+
+@gpu
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("M,H,F", [(1, 8, 8), (3, 72, 40), (130, 200, 264), (65, 1288, 136), (2100, 136, 4104)])
+def test_contractions_that_are_no_multiple_of_64(M, H, F, act):
+    _forward(M, H, F, act)
+    _forward(M, H, F, act, bias=False, save=False)
+    _backward(M, H, F, act)
+
+
+@gpu
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("M,H,F", [(1, 1280, 8), (1, 2048, 2056), (7, 1024, 264), (200, 1280, 2056), (65, 2048, 2056)])
+def test_split_contractions(M, H, F, act):
+    assert B.linear_plan(B.LAYOUT_FWD_GELU, M, 2 * F, H)[2] > 1 and B.linear_plan(B.LAYOUT_DGRAD_GELU, M, F, H)[2] > 1
+    for split in (True, False):
+        _forward(M, H, F, act, split=split)
+        _forward(M, H, F, act, bias=False, save=False, split=split)
+        _backward(M, H, F, act, split=split)
+
+
+@gpu
+def test_extreme_gates():
+    """Gates far out on both sides: the activation is g or 0, never NaN."""
+    M, H, F = 64, 64, 64
+    announce("glu extreme gates")
+    y = torch.zeros(M, H)
+    y[:, 0] = torch.linspace(-60000.0, 60000.0, M)
+    w = torch.zeros(2 * F, H)
+    w[:F, 0], w[F:, 1], y[:, 1] = 1.0, 1.0, 0.5
+    y, w = y.to(BF), w.to(BF)
+    for act, code in ACTS.items():
+        gu, h = B.enc_glu_up_fwd(cuda(y), cuda(w), act=code)
+        with np.errstate(over="ignore"):
+            rgu, rh, gb, hb = P.glu_fwd(f64(y), f64(w), None, act)
+        _within(h, rh, hb + 1e-30, act)
+        dgu = B.enc_glu_down_bwd_data(cuda(torch.eye(M, H).to(BF)), cuda(torch.ones(H, F).to(BF)), gu, act=code)
+        with np.errstate(over="ignore"):
+            ref, bound = P.glu_bwd(np.eye(M, H), np.ones((H, F)), f64(gu), act)
+        _within(dgu, ref, bound, act)
+
+
+@gpu
+def test_products_replay_from_a_graph_and_repeat_bit_for_bit():
+    M, H, F = 300, 1280, 776  # split and unsplit products
+    announce("glu graph")
+    y, w, w2, dout = (cuda(random_bf16(s, i, c)) for i, (s, c) in enumerate(
+        [((M, H), 1.0), ((2 * F, H), 0.03), ((H, F), 0.03), ((M, H), 1.0)]))
+    need = max(B.linear_workspace_bytes(M, 2 * F, H), B.linear_workspace_bytes(M, F, H),
+               B.linear_workspace_bytes(M, H, 2 * F))
+    ws = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
+    outs = [torch.empty(s, dtype=BF, device="cuda") for s in ((M, 2 * F), (M, F), (M, 2 * F), (M, H))]
+    dw, db = torch.empty(2 * F, H, device="cuda"), torch.empty(2 * F, device="cuda")
+    wws = torch.empty(max(B.linear_bwd_weight_workspace_bytes(M, 2 * F, H), 16), dtype=torch.uint8, device="cuda")
+
+    def chain():
+        gu, h, dgu, dy = outs
+        B.enc_glu_up_fwd(y, w, act=B.GLU_SILU, gu=gu, h=h, ws=ws)
+        B.enc_glu_down_bwd_data(dout, w2, gu, act=B.GLU_SILU, dgu=dgu, ws=ws)
+        B.enc_glu_up_bwd_data(dgu, w, dy2=dy, ws=ws)
+        B.enc_glu_up_bwd_weight(dgu, y, dw, db, ws=wws)
+
+    bits = lambda: [t.clone().view(torch.int16) for t in outs] + [t.clone().view(torch.int32) for t in (dw, db)]  # noqa: E731
+    chain()
+    want = bits()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        chain()
+    for _ in range(3):
+        for t in outs + [dw, db]:
+            t.fill_(0.25)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(bits(), want))
+        chain()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(bits(), want))
+    # the weight gradient is the general product
+    rw, rb = B.enc_linear_bwd_weight(outs[2], y)
+    assert torch.equal(rw, dw) and torch.equal(rb, db)
