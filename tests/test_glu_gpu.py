@@ -19,7 +19,7 @@ ACTS = {"silu": B.GLU_SILU, "gelu": B.GLU_GELU}
 # the products are offered runs, in every phase of its ring
 SIZES = sorted([(1, 8), (40, 72), (120, 200), (300, 520), (257, 1000), (200, 4224), (776, 1304), (1030, 2056),
                 (6570, 264), (6570, 528), (2050, 1032), (5400, 528), (980, 5544), (1500, 2056), (4100, 1032),
-                (7350, 528), (7610, 792), (1030, 5504), (2050, 4008), (7610, 1584)], key=lambda s: s[0] * s[1])
+                (7350, 528), (7610, 792), (1030, 5504), (2050, 4008), (7610, 1584), (1760, 6600)], key=lambda s: s[0] * s[1])
 STEPS = (1, 2, 3, 4, 5, 8, 20)
 
 
