@@ -517,8 +517,8 @@ int enc_attn_packed_fwd(int tokens, int seqs, int heads, int kv_heads, int head_
 /* [Packed block step: backward of the self-attention within each sequence]
  * Exact gradient of enc_attn_packed_fwd, P recomputed from lse; dK and dV are
  * summed over the heads that share them.  dqkv: [tokens, (heads + 2 kv_heads)
- * * head_dim]; rows of no sequence keep what dqkv held.  ws: fp32 D vector
- * (enc_attn_packed_bwd_workspace_bytes).  No atomics, deterministic. */
+ * * head_dim]; rows of no sequence keep what dqkv held.  ws: two fp32
+ * vectors (enc_attn_packed_bwd_workspace_bytes).  No atomics, deterministic. */
 int enc_attn_packed_bwd_workspace_bytes(int tokens, int heads, size_t *bytes);
 int enc_attn_packed_bwd(int tokens, int seqs, int heads, int kv_heads, int head_dim, int causal, const void *plan,
                         size_t plan_bytes, const enc_bf16 *qkv, const enc_bf16 *o, const float *lse,

@@ -1098,7 +1098,8 @@ int enc_attn_packed_bwd(int tokens, int seqs, int heads, int kv_heads, int head_
   a.tokens = tokens, a.slots = packed_slots(tokens, seqs), a.heads = heads, a.kv_heads = kv_heads, a.d = head_dim;
   a.causal = causal, a.plan = static_cast<const PackedPlan *>(plan), a.qkv = qkv;
   a.o = const_cast<enc_bf16 *>(o), a.lse = const_cast<float *>(lse);  // read only in the backward
-  a.dO = do_, a.dqkv = dqkv, a.dvec = static_cast<float *>(ws);
+  a.dO = do_, a.dqkv = dqkv, a.nlse = static_cast<float *>(ws);
+  a.ndvec = a.nlse + attn_packed_bwd_vec(tokens, heads);
   if (!launch_attn_packed_bwd(a, as_stream(stream))) return refused_after_checks(fn);
   return launched(fn);
 }

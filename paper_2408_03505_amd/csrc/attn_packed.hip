@@ -94,6 +94,42 @@ __device__ __forceinline__ void packed_issue(const bf16_t *src, int rows, int ld
     buffer_load_lds16(rsrc, __builtin_amdgcn_readfirstlane(lds_tile + (wid * N + i) * 1024), voff[i], 0);
 }
 
+// The two read patterns of a tile (TileReads) from whole LDS addresses, so that
+// stage, tile, fragment and step all go in the reads' offset field, and reads
+// of fp32 vectors in the order of a result's registers.  The tile swizzle is an
+// XOR of the 16-byte chunk, so steps along the columns are an XOR of the first
+// one's address: one vector instruction per read and two registers in all,
+// where registers are what limits the kernel.
+template <int D, bool PERM>
+struct PackedReads {
+  int row0, col0, vec0;
+  __device__ __forceinline__ void init(int lane, uint32_t lds0) {
+    row0 = lds0 + tile_off(lane & 31, lane >> 5);
+    const int k = (PERM ? 4 : 8) * (lane >> 5) + ((lane & 15) >> 2);
+    const int n = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+    col0 = lds0 + tile_off(k, n >> 3) + (n & 7) * 2;
+    vec0 = lds0 + (lane >> 5) * 16;
+    asm volatile("" : "+v"(row0), "+v"(col0), "+v"(vec0));
+  }
+  // Called in the loop: keeps its addresses from being computed, and held in
+  // registers, outside it.
+  __device__ __forceinline__ void local() { asm volatile("" : "+v"(row0), "+v"(col0)); }
+  template <class T>
+  __device__ static __forceinline__ T at(uint32_t addr) {
+    return *reinterpret_cast<const __attribute__((address_space(3))) T *>(addr);
+  }
+  __device__ __forceinline__ bf16x8_t row(int base, int f, int kk) const {
+    return at<bf16x8_t>((row0 ^ (kk << 5)) + base + f * 32 * kDL * 2);
+  }
+  // the second read: 8 rows further with PERM (tsw differs in one bit), else 4
+  __device__ __forceinline__ bf16x8_t col(int base, int nf, int st) const {
+    const int o = base + st * 16 * kDL * 2, c = col0 ^ (nf << 6);
+    const int c1 = PERM ? (c ^ 32) + 8 * kDL * 2 : (c ^ 16) + 4 * kDL * 2;
+    return lds_read_tr(reinterpret_cast<const lds_char *>(c + o), reinterpret_cast<const lds_char *>(c1 + o));
+  }
+  __device__ __forceinline__ f32x4_t vec(int base) const { return at<f32x4_t>(vec0 + base); }
+};
+
 // ------------------------------------------------------------------ forward
 
 template <int D, int KT, int MINB>
@@ -272,7 +308,10 @@ __global__ __launch_bounds__(NW * 64, MINB) void packed_bwd_dq_kernel(PackedAttn
   dd += __shfl_xor(dd, 32, kWave);
   const float c = kLog2e / sqrtf(static_cast<float>(D));
   const float lse2 = qvalid ? p.lse[vec] * kLog2e : 0.f;
-  if (qvalid && hf == 0) p.dvec[vec] = dd;
+  if (qvalid && hf == 0) {
+    p.nlse[vec] = -p.lse[vec] * sqrtf(static_cast<float>(D));
+    p.ndvec[vec] = -dd;
+  }
 
   f32x16_t acc[H::NF];
 #pragma unroll
@@ -337,48 +376,60 @@ __global__ __launch_bounds__(NW * 64, MINB) void packed_bwd_dq_kernel(PackedAttn
 
 // ------------------------------------------------------------------ backward: dK, dV
 //
-// Two waves share each group of 32 keys: wave A computes S = Q K^T, P and
-// dV^T += dO^T P, wave B dP = dO V^T, dS and dK^T += Q^T dS; P goes from A to
-// B through LDS in fp32, in the MFMA result layout both waves hold.  An item's
-// kPackedRows keys are kPackedRows / (32 NG) workgroups.
+// Each wave owns 32 keys and keeps their K and V rows and both accumulators in
+// registers.  Per tile of 32 queries: S = Q K^T and dP = dO V^T, P, dS, then
+// dV^T += dO^T P and dK^T += Q^T dS, 32 products of 32x32x16 at D = 128 to 48
+// full-rate vector instructions and 16 exponentials.  The accumulators of S and
+// dP start from the dQ kernel's -lse sqrt(D) and -D_i, which lie in LDS in the
+// order of the result's registers, so neither is subtracted afterwards.
 
-// LDS of one stage: the Q and dO tiles, then lse and D of up to 64 queries.
+// LDS of one stage: the Q and dO tiles, then -lse sqrt(D) and -D_i of up to 64 queries.
 template <int KT>
 constexpr int packed_dkdv_stage() {
   return 2 * tile_bytes<KT>() + 2 * 64 * 4;
 }
 
-template <int D, int NG, int KT, int MINB>
-__global__ __launch_bounds__(NG * 128, MINB) void packed_bwd_dkdv_kernel(PackedAttnArgs p) {
+// Wide heads keep the V rows in LDS: K, V and the two accumulators would leave
+// no registers to read operands ahead into.
+constexpr bool dkdv_v_in_lds(int d) { return d > 80; }
+
+template <int D, int NW, int KT, int MINB>
+__global__ __launch_bounds__(NW * 64, MINB) void packed_bwd_dkdv_kernel(PackedAttnArgs p) {
   using H = Head<D>;
-  constexpr int NW = 2 * NG, TB = tile_bytes<KT>(), NL = TileLoads<KT, NW>::N, TILES = 2 * TB;  // Q, dO
-  constexpr int SUBS = kPackedRows / (32 * NG);   // workgroups per item
-  constexpr int STAGE = packed_dkdv_stage<KT>();  // + lse, D
-  constexpr int PX = 2 * STAGE;                   // P hand-over: one 32 x KT fp32 slot per key group
+  static_assert(32 * NW == kPackedRows, "one item per workgroup");
+  constexpr int TB = tile_bytes<KT>(), NL = TileLoads<KT, NW>::N, TILES = 2 * TB;  // Q, dO
+  constexpr int STAGE = packed_dkdv_stage<KT>(), NS = KT / 32;
+  constexpr bool VL = dkdv_v_in_lds(D);
   extern __shared__ __attribute__((aligned(1024))) char smem_raw[];
   const lds_char *smem = (const lds_char *)(smem_raw);
   const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(smem));
 
   int item, kvh, first, len, row;
   packed_item(p.kv_heads, item, kvh);
-  if (!load_item(p.plan, p.slots, p.tokens, item / SUBS, first, len, row)) return;
-  row += item % SUBS * 32 * NG;  // the workgroup's first key
-  if (row >= len) return;
+  if (!load_item(p.plan, p.slots, p.tokens, item, first, len, row)) return;
   const int group = p.heads / p.kv_heads;
   const int A = p.heads * D, ld = A + 2 * p.kv_heads * D;
   const int lane = threadIdx.x & 63, hf = lane >> 5;
   const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const bool role_a = wid < NG;  // wave-uniform
-  const int grp = role_a ? wid : wid - NG;
-  const int k0w = row + grp * 32;
+  const int k0w = row + wid * 32;
   const bool active = k0w < len;  // wave-uniform
   const int key = k0w + (lane & 31);
   const bf16_t *seq = p.qkv + static_cast<size_t>(first) * ld;
   const bf16_t *dseq = p.dO + static_cast<size_t>(first) * A;
 
-  uint32_t vq[NL], vd[NL];
-  packed_voff<D, KT, NW>(vq, wid, lane, ld, false);
-  packed_voff<D, KT, NW>(vd, wid, lane, A, false);
+  // Two loads per tile and wave, the second four rows further, where the swizzle
+  // swaps neighbouring chunks: its offset is made from the first one's when it
+  // is needed (rows are multiples of 32 bytes).
+  static_assert(NL == 2, "two loads per tile and wave");
+  uint32_t v0[NL];
+  packed_voff<D, KT, NW>(v0, wid, lane, ld, false);
+  const uint32_t vq = v0[0];
+  packed_voff<D, KT, NW>(v0, wid, lane, A, false);
+  const uint32_t vd = v0[0];
+  auto load2 = [&](const bf16_t *src, int rows, int rld, uint32_t lds_tile, uint32_t v) {
+    const uint32_t both[2] = {v, (v ^ 16) + static_cast<uint32_t>(8 * rld)};
+    packed_issue<D, KT, NW>(src, rows, rld, lds_tile, both, wid);
+  };
   // query tiles t0 .. nq - 1 of each of the group's heads in turn
   const int t0 = p.causal ? row / KT : 0, nq = (len + KT - 1) / KT;
   const int total = (nq - t0) * group;
@@ -386,110 +437,93 @@ __global__ __launch_bounds__(NG * 128, MINB) void packed_bwd_dkdv_kernel(PackedA
   auto issue = [&](int n) {
     const uint32_t buf = lds0 + (n & 1) * STAGE;
     const int rem = len - it * KT;
-    packed_issue<D, KT, NW>(seq + static_cast<size_t>(it) * KT * ld + ih * D, rem, ld, buf, vq, wid);
-    packed_issue<D, KT, NW>(dseq + static_cast<size_t>(it) * KT * A + ih * D, rem, A, buf + TB, vd, wid);
-    // lse (wave 0) and D (wave 1) of the tile's queries; those past the
-    // sequence read as zero: their Q and dO are zero too, so P = 1 meets zeros
+    load2(seq + static_cast<size_t>(it) * KT * ld + ih * D, rem, ld, buf, vq);
+    load2(dseq + static_cast<size_t>(it) * KT * A + ih * D, rem, A, buf + TB, vd);
+    // the tile's vectors; past the sequence they read as zero, as Q and dO do:
+    // P = 1 then meets zeros only
     const size_t vec = static_cast<size_t>(ih) * p.tokens + first + it * KT;
     const uint32_t ext = static_cast<uint32_t>(min(rem, KT)) * 4;
     if (wid == 0)
-      buffer_load_lds4(make_rsrc(p.lse + vec, ext), __builtin_amdgcn_readfirstlane(buf + TILES), lane * 4, 0);
+      buffer_load_lds4(make_rsrc(p.nlse + vec, ext), __builtin_amdgcn_readfirstlane(buf + TILES), lane * 4, 0);
     if (wid == 1)
-      buffer_load_lds4(make_rsrc(p.dvec + vec, ext), __builtin_amdgcn_readfirstlane(buf + TILES + 64 * 4), lane * 4,
+      buffer_load_lds4(make_rsrc(p.ndvec + vec, ext), __builtin_amdgcn_readfirstlane(buf + TILES + 64 * 4), lane * 4,
                        0);
     if (++it == nq) it = t0, ++ih;
   };
 
-  // K rows (wave A) or V rows (wave B) of this lane's key
-  bf16x8_t rf[H::KS];
-  load_row_operand<D>(rf, seq + static_cast<size_t>(key) * ld + A + (role_a ? kvh : p.kv_heads + kvh) * D, key < len,
-                      hf);
-
-  f32x16_t acc[H::NF];  // dV^T (wave A) or dK^T (wave B)
+  bf16x8_t kf[H::KS], vf[H::KS];
+  const uint32_t vown = lds0 + 2 * STAGE + wid * (32 * D * 2) + lane * 16;  // this lane's V row, VL
+  {
+    const bf16_t *kp = seq + static_cast<size_t>(key) * ld + A + kvh * D;
+    load_row_operand<D>(kf, kp, key < len, hf);
+    load_row_operand<D>(vf, kp + p.kv_heads * D, key < len, hf);
+    if constexpr (VL) {
 #pragma unroll
-  for (int i = 0; i < H::NF; ++i) acc[i] = f32x16_t{};
-  constexpr int NS = KT / 32;  // 32-query fragments per tile
-  // P hand-over slot of this key group: lane l's 16 NS values as 16-byte
-  // chunks, chunk j at position j ^ pswz(l) (distinct banks over any 16 lanes)
-  f32x4_t *pxl = reinterpret_cast<f32x4_t *>(smem_raw + PX) + grp * (8 * KT) + lane * (4 * NS);
-  const int pswz = (lane >> (NS == 1 ? 2 : 1)) & (4 * NS - 1);
+      for (int kk = 0; kk < H::KS; ++kk)
+        *reinterpret_cast<__attribute__((address_space(3))) bf16x8_t *>(vown + kk * 1024) = vf[kk];
+    }
+  }
+  f32x16_t dk[H::NF], dv[H::NF];
+#pragma unroll
+  for (int i = 0; i < H::NF; ++i) dk[i] = f32x16_t{}, dv[i] = f32x16_t{};
   const float c = kLog2e / sqrtf(static_cast<float>(D));
-  // wave A: row reads of Q, column reads of dO; wave B the other way round
-  TileReads<D, true> reads;
-  reads.init(lane, role_a ? 0 : TB, role_a ? TB : 0);
+  PackedReads<D, true> rd;
+  rd.init(lane, lds0);
   issue(0);
   int ct = t0;  // the tile computed next
   auto tile = [&](auto stage, int n) {
+    constexpr int ST = stage.value * STAGE;
     wait_vmcnt<0>();  // this wave's loads of tile n
     // every wave's loads of tile n have landed, and every wave is done with
-    // tile n - 1: its buffer is refilled next and its P slots rewritten
+    // tile n - 1, whose buffer is refilled next
     block_barrier();
     if (n + 1 < total) issue(n + 1);
-    const lds_char *Ts = smem + stage.value * STAGE;
-    const float *Ls = reinterpret_cast<const float *>(smem_raw + stage.value * STAGE + TILES);
     const int q0 = ct * KT;
     if (++ct == nq) ct = t0;
     // waves whose keys all lie past the sequence, or (causal) behind every
-    // query of the tile, only load and synchronise; both waves of a key group
-    // agree
-    const bool work = active && !(p.causal && q0 + KT <= k0w);
-    const bool diag = p.causal && q0 < k0w + 31;  // some query of the tile precedes some key of the wave
-    // dO^T (wave A) or Q^T (wave B) operands of the token-contracting
-    // product, read while S or dP and the P hand-over run
-    ColOperands<D, KT, (D <= kPrefetchMaxD), true> cop;
-    f32x16_t sv[NS];
-    if (work) {
-      cop.fetch(Ts, reads);
-      // S^T (wave A) or dP^T (wave B): register 4g+e of fragment f is query
-      // f*32 + 8g + 4hf + e (four consecutive queries)
+    // query of the tile, only load and synchronise
+    if (!active || (p.causal && q0 + KT <= k0w)) return;
+    rd.local();
+    // register 4g+e of fragment f is query f*32 + 8g + 4hf + e
+    f32x16_t s[NS], dp[NS];
 #pragma unroll
-      for (int f = 0; f < NS; ++f) {
-        sv[f] = f32x16_t{};
+    for (int f = 0; f < NS; ++f) {
 #pragma unroll
-        for (int kk = 0; kk < H::KS; ++kk) sv[f] = mfma32(reads.row(Ts, f, kk), rf[kk], sv[f]);
+      for (int g = 0; g < 4; ++g) {
+        const f32x4_t l4 = rd.vec(ST + TILES + f * 128 + g * 32), d4 = rd.vec(ST + TILES + 256 + f * 128 + g * 32);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[f][4 * g + e] = l4[e], dp[f][4 * g + e] = d4[e];
       }
-      if (role_a) {
 #pragma unroll
-        for (int f = 0; f < NS; ++f)
+      for (int kk = 0; kk < H::KS; ++kk) s[f] = mfma32(rd.row(ST, f, kk), kf[kk], s[f]);
 #pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            const int qi = f * 32 + 8 * g + 4 * hf;
-            const f32x4_t l4 = *reinterpret_cast<const f32x4_t *>(Ls + qi) * kLog2e;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              float pv = exp2_hw(__builtin_fmaf(sv[f][4 * g + e], c, -l4[e]));
-              if (diag && q0 + qi + e < key) pv = 0.f;
-              sv[f][4 * g + e] = pv;
-            }
-            pxl[(f * 4 + g) ^ pswz] = f32x4_t{sv[f][4 * g], sv[f][4 * g + 1], sv[f][4 * g + 2], sv[f][4 * g + 3]};
-          }
-      }
+      for (int kk = 0; kk < H::KS; ++kk)
+        dp[f] = mfma32(rd.row(ST + TB, f, kk), VL ? rd.template at<bf16x8_t>(vown + kk * 1024) : vf[kk], dp[f]);
     }
-    lds_barrier();  // P of every group is in LDS
-    if (work) {
-      if (!role_a) {
 #pragma unroll
-        for (int f = 0; f < NS; ++f)
+    for (int f = 0; f < NS; ++f)
 #pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            const int qi = f * 32 + 8 * g + 4 * hf;
-            const f32x4_t d4 = *reinterpret_cast<const f32x4_t *>(Ls + 64 + qi);
-            const f32x4_t p4 = pxl[(f * 4 + g) ^ pswz];
+      for (int i = 0; i < 16; ++i) s[f][i] = exp2_hw(s[f][i] * c);  // P
+    if (p.causal && q0 < k0w + 31) {  // some query of the tile precedes some key of the wave
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              float ds = p4[e] * (sv[f][4 * g + e] - d4[e]);  // dS^T
-              if (diag && q0 + qi + e < key) ds = 0.f;
-              sv[f][4 * g + e] = ds;
-            }
-          }
-      }
-      // dV^T += dO^T P (wave A) or dK^T += Q^T dS (wave B)
+      for (int f = 0; f < NS; ++f)
 #pragma unroll
-      for (int st = 0; st < KT / 16; ++st) {
-        const bf16x8_t pb = pack8(sv[st >> 1], st & 1);
+        for (int i = 0; i < 16; ++i)
+          if (q0 + f * 32 + (i >> 2) * 8 + hf * 4 + (i & 3) < key) s[f][i] = 0.f;
+    }
 #pragma unroll
-        for (int nf = 0; nf < H::NF; ++nf) acc[nf] = mfma32(cop.get(Ts, reads, nf, st), pb, acc[nf]);
-      }
+    for (int st = 0; st < KT / 16; ++st) {
+      const bf16x8_t pb = pack8(s[st >> 1], st & 1);
+#pragma unroll
+      for (int nf = 0; nf < H::NF; ++nf) dv[nf] = mfma32(rd.col(ST + TB, nf, st), pb, dv[nf]);
+    }
+#pragma unroll
+    for (int f = 0; f < NS; ++f) dp[f] *= s[f];  // dS
+#pragma unroll
+    for (int st = 0; st < KT / 16; ++st) {
+      const bf16x8_t sb = pack8(dp[st >> 1], st & 1);
+#pragma unroll
+      for (int nf = 0; nf < H::NF; ++nf) dk[nf] = mfma32(rd.col(ST, nf, st), sb, dk[nf]);
     }
   };
   for (int n = 0; n < total; n += 2) {
@@ -497,18 +531,17 @@ __global__ __launch_bounds__(NG * 128, MINB) void packed_bwd_dkdv_kernel(PackedA
     if (n + 1 < total) tile(Stage<1>(), n + 1);
   }
   block_barrier();  // the output slots reuse the tile buffers
-  // wave A holds dV, wave B dK
-  bf16_t *out = p.dqkv + static_cast<size_t>(first + k0w) * ld + A + (role_a ? p.kv_heads + kvh : kvh) * D;
-  store_dmajor_lds<D>(out, ld, acc, role_a ? 1.0f : 1.0f / sqrtf(static_cast<float>(D)), lane,
-                      const_cast<lds_char *>(smem) + wid * 8192, len - k0w);
+  bf16_t *out = p.dqkv + static_cast<size_t>(first + k0w) * ld + A + kvh * D;
+  lds_char *slot = const_cast<lds_char *>(smem) + wid * 8192;
+  store_dmajor_lds<D>(out, ld, dk, 1.0f / sqrtf(static_cast<float>(D)), lane, slot, len - k0w);
+  store_dmajor_lds<D>(out + p.kv_heads * D, ld, dv, 1.0f, lane, slot, len - k0w);
 }
 
-// Launch shapes, as for the dense kernels: forward and dQ run 4 waves of 32
-// queries, dK/dV two groups of 32 keys with two waves each; KT is the token
-// tile streamed through LDS, MINB the workgroups each CU must hold at once.
+// Launch shapes: 4 waves of 32 queries (forward, dQ) or keys (dK/dV); KT is the
+// token tile streamed through LDS, MINB the workgroups each CU must hold at once.
 constexpr int kFwdKT = 32, kFwdMinBlocks = 3, kFwdSmallGrid = 256;
 constexpr int kDqWaves = 4, kDqKT = 32, kDqMinBlocks = 2;
-constexpr int kDkvGroups = 2, kDkvKT = 32, kDkvMinBlocks = 3;
+constexpr int kDkvWaves = 4, kDkvKT = 32, kDkvMinBlocks = 2;
 
 template <int D, int KT, int MINB>
 void launch_fwd_cfg(const PackedAttnArgs &a, hipStream_t s) {
@@ -530,13 +563,12 @@ void launch_fwd_d(const PackedAttnArgs &a, hipStream_t s) {
 template <int D>
 void launch_bwd_d(const PackedAttnArgs &a, hipStream_t s) {
   constexpr int kDqLds = std::max(4 * tile_bytes<kDqKT>(), kDqWaves * 8192);
-  constexpr int kDkvLds = std::max(2 * packed_dkdv_stage<kDkvKT>() + kDkvGroups * 32 * kDkvKT * 4,
-                                   2 * kDkvGroups * 8192);
+  constexpr int kDkvLds =
+      std::max(2 * packed_dkdv_stage<kDkvKT>() + (dkdv_v_in_lds(D) ? kDkvWaves * 32 * D * 2 : 0), kDkvWaves * 8192);
   hipLaunchKernelGGL((packed_bwd_dq_kernel<D, kDqWaves, kDqKT, kDqMinBlocks>), dim3(a.slots * a.heads),
                      dim3(kDqWaves * 64), kDqLds, s, a);
-  hipLaunchKernelGGL((packed_bwd_dkdv_kernel<D, kDkvGroups, kDkvKT, kDkvMinBlocks>),
-                     dim3(a.slots * a.kv_heads * (kPackedRows / (32 * kDkvGroups))), dim3(kDkvGroups * 128), kDkvLds,
-                     s, a);
+  hipLaunchKernelGGL((packed_bwd_dkdv_kernel<D, kDkvWaves, kDkvKT, kDkvMinBlocks>), dim3(a.slots * a.kv_heads),
+                     dim3(kDkvWaves * 64), kDkvLds, s, a);
 }
 
 }  // namespace

@@ -76,9 +76,13 @@ inline size_t packed_plan_bytes(int tokens, int seqs) {
   return (b + 255) & ~static_cast<size_t>(255);
 }
 
-// ---- Packed attention backward: the D vector, one fp32 per head and row.
+// ---- Packed attention backward: two fp32 vectors, one value per head and row
+// (each starts on a 16-byte boundary).
+inline size_t attn_packed_bwd_vec(int tokens, int heads) {
+  return (static_cast<size_t>(heads) * tokens + 3) & ~static_cast<size_t>(3);
+}
 inline size_t attn_packed_bwd_ws_bytes(int tokens, int heads) {
-  return static_cast<size_t>(heads) * tokens * sizeof(float);
+  return 2 * attn_packed_bwd_vec(tokens, heads) * sizeof(float);
 }
 
 // ---- GEMM tile choice.  The direct-to-LDS kernels come in these output

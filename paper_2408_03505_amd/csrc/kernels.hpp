@@ -138,7 +138,8 @@ struct PackedAttnArgs {
   float *lse;         // [heads, tokens]
   const bf16_t *dO;
   bf16_t *dqkv;
-  float *dvec;  // [heads, tokens]
+  // backward workspace, [heads, tokens] each: -lse sqrt(d) and -D_i
+  float *nlse, *ndvec;
 };
 bool launch_attn_packed_fwd(const PackedAttnArgs &a, hipStream_t s);
 bool launch_attn_packed_bwd(const PackedAttnArgs &a, hipStream_t s);

@@ -79,7 +79,7 @@ def test_plan_sizes():
     for tokens, seqs in ((1, 1), (128, 1), (129, 7), (100000, 40), (2 ** 31 - 1, 65536)):
         items = tokens // 128 + seqs
         assert B.packed_plan_bytes(tokens, seqs) == (16 * (1 + items) + 255) // 256 * 256
-    assert B.attn_packed_bwd_workspace_bytes(1000, 12) == 48000
+    assert B.attn_packed_bwd_workspace_bytes(1000, 12) == 96000  # two vectors
     n = ctypes.c_size_t()
     assert _st("enc_attn_packed_bwd_workspace_bytes", 2 ** 30, 4, ctypes.byref(n)) == UNS
     assert _st("enc_attn_packed_bwd_workspace_bytes", 0, 4, ctypes.byref(n)) == INV
@@ -97,7 +97,7 @@ def test_attention_refusals():
         big[0], big[1], big[2], big[3] = 8, 65536, 128, 128
         assert _st(name, *big) == UNS
         _pointers(name, base)
-    _bad("enc_attn_packed_bwd", BWD, [(14, 64 * 4 * 4 - 1, WSP)])
+    _bad("enc_attn_packed_bwd", BWD, [(14, 2 * 64 * 4 * 4 - 1, WSP)])
 
 
 @no_gpu_only
