@@ -77,29 +77,64 @@ __device__ __forceinline__ void packed_voff(uint32_t (&v)[N], int wid, int lane,
   }
 }
 
-// Extent in bytes of `rows` rows from a head's first column, at most one tile.
-template <int D, int KT>
-__device__ __forceinline__ uint32_t tile_extent(int rows, int ld) {
-  return static_cast<uint32_t>((min(rows, KT) - 1) * ld + D) * 2;
-}
+// One tensor's tiles of one sequence and head, loaded in order: a buffer
+// resource from the head's first column in the first row on, which ends with
+// the sequence's last row, and the next tile's byte offset in it.  A load is
+// then one addition and two instructions per kilobyte: set up anew for each
+// tile, the loads' scalar instructions held each wave up by a tenth of its time.
+template <int D, int KT, int NW>
+struct PackedLoads {
+  static constexpr int NL = TileLoads<KT, NW>::N;
+  u32x4_t rsrc;
+  uint32_t voff[NL], soff, step, wbase;
+  __device__ __forceinline__ void init(const bf16_t *src, int rows, int ld, uint32_t lds_base, int wid, int lane,
+                                       bool perm) {
+    packed_voff<D, KT, NW>(voff, wid, lane, ld, perm);
+    step = static_cast<uint32_t>(KT) * ld * 2;
+    wbase = __builtin_amdgcn_readfirstlane(lds_base + wid * NL * 1024);
+    start(src, rows, ld);
+  }
+  // the next tile is the one at src, of `rows` rows to the sequence's end
+  __device__ __forceinline__ void start(const bf16_t *src, int rows, int ld) {
+    rsrc = make_rsrc(src, (static_cast<uint32_t>(rows - 1) * ld + D) * 2);
+    soff = 0;
+  }
+  // into the tile OFF bytes on in LDS
+  template <int OFF>
+  __device__ __forceinline__ void issue() {
+    issue_each<OFF, 0>();
+    soff += step;
+  }
+  template <int OFF, int I>
+  __device__ __forceinline__ void issue_each() const {
+    if constexpr (I < NL) {
+      issue_lds16<OFF + I * 1024>(rsrc, wbase, voff[I], soff);
+      issue_each<OFF, I + 1>();
+    }
+  }
+};
 
-// Loads the tile at `src` (a head's first column in the tile's first row),
-// `rows` rows of which are the sequence's.
-template <int D, int KT, int NW, int N>
-__device__ __forceinline__ void packed_issue(const bf16_t *src, int rows, int ld, uint32_t lds_tile,
-                                             const uint32_t (&voff)[N], int wid) {
-  const u32x4_t rsrc = make_rsrc(src, tile_extent<D, KT>(rows, ld));
-#pragma unroll
-  for (int i = 0; i < N; ++i)
-    buffer_load_lds16(rsrc, __builtin_amdgcn_readfirstlane(lds_tile + (wid * N + i) * 1024), voff[i], 0);
-}
+// TileReads with every address a whole LDS address, so that stage, tile,
+// fragment and step all go in the reads' offset field.
+template <int D, bool PERM>
+struct PackedReadsR {
+  TileReads<D, PERM> t;
+  __device__ __forceinline__ void init(int lane, uint32_t lds0) { t.init(lane, lds0, lds0); }
+  __device__ __forceinline__ bf16x8_t row(int base, int f, int kk) const {
+    return *reinterpret_cast<const __attribute__((address_space(3))) bf16x8_t *>(
+        static_cast<uint32_t>(t.row_off[kk] + base + f * 32 * kDL * 2));
+  }
+  __device__ __forceinline__ bf16x8_t col(int base, int nf, int st) const {
+    const int o = base + st * 16 * kDL * 2;
+    return lds_read_tr(reinterpret_cast<const lds_char *>(static_cast<uint32_t>(t.col_off[nf][0] + o)),
+                       reinterpret_cast<const lds_char *>(static_cast<uint32_t>(t.col_off[nf][1] + o)));
+  }
+};
 
-// The two read patterns of a tile (TileReads) from whole LDS addresses, so that
-// stage, tile, fragment and step all go in the reads' offset field, and reads
-// of fp32 vectors in the order of a result's registers.  The tile swizzle is an
-// XOR of the 16-byte chunk, so steps along the columns are an XOR of the first
-// one's address: one vector instruction per read and two registers in all,
-// where registers are what limits the kernel.
+// The same, and reads of fp32 vectors in the order of a result's registers,
+// from few registers.  The tile swizzle is an XOR of the 16-byte chunk, so steps
+// along the columns are an XOR of the first one's address: one vector
+// instruction per read, where registers are what limits the kernel.
 template <int D, bool PERM>
 struct PackedReads {
   int row0, col0, vec0;
@@ -131,14 +166,44 @@ struct PackedReads {
 };
 
 // ------------------------------------------------------------------ forward
+//
+// Each wave runs one tile ahead of itself: the products S(t + 1) = K Q^T are in
+// one straight piece of code with the exponentials of tile t, and the running
+// maximum of tile t + 1 with the products O += P V of tile t, so that vector
+// instructions fill the time that a matrix instruction leaves the SIMD's issue
+// free.  (Left to different waves they hardly overlap: with S, softmax and PV in
+// turn and three waves per SIMD, the matrix cores were busy 0.45 of the time and
+// the vector units 0.45.)  Tile t + 2's keys and tile t + 1's values are loaded
+// meanwhile.
 
-template <int D, int KT, int MINB>
-__global__ __launch_bounds__(256, MINB) void packed_fwd_kernel(PackedAttnArgs p) {
+// The next N instructions of a kind in the order wanted of the scheduler.
+constexpr int kSchedVector = 0x2, kSchedMfma = 0x8, kSchedLds = 0x100, kSchedTrans = 0x400;
+template <int KIND, int N>
+__device__ __forceinline__ void sched_group() {
+  __builtin_amdgcn_sched_group_barrier(KIND, N, 0);
+}
+
+__device__ __forceinline__ float max_halves(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+__device__ __forceinline__ float max16(const f32x16_t &s) {
+  float a = fmaxf(s[0], s[1]), b = fmaxf(s[8], s[9]);
+#pragma unroll
+  for (int i = 2; i < 8; ++i) a = fmaxf(a, s[i]), b = fmaxf(b, s[i + 8]);
+  return fmaxf(a, b);
+}
+
+template <int D, int WPE>
+__global__ __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_waves_per_eu(WPE, WPE))) void
+packed_fwd_kernel(PackedAttnArgs p) {
   using H = Head<D>;
-  constexpr int TB = tile_bytes<KT>(), NL = TileLoads<KT, 4>::N;
-  extern __shared__ __attribute__((aligned(1024))) char smem_raw[];  // 2 x (K tile, V tile)
-  const lds_char *smem = (const lds_char *)(smem_raw);
-  const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(smem));
+  constexpr int KT = 32, TB = tile_bytes<KT>(), VB = 2 * TB;  // K, K, V, V
+  using Loads = PackedLoads<D, KT, 4>;
+  constexpr int NL = Loads::NL;
+  extern __shared__ __attribute__((aligned(1024))) char smem_raw[];
+  const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((const lds_char *)smem_raw));
 
   int item, h, first, len, row;
   packed_item(p.heads, item, h);
@@ -149,19 +214,12 @@ __global__ __launch_bounds__(256, MINB) void packed_fwd_kernel(PackedAttnArgs p)
   const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int q0 = row + wid * 32;  // the wave's first query
   const int q = q0 + (lane & 31);
-  const bool active = q0 < len;  // wave-uniform
   const bf16_t *seq = p.qkv + static_cast<size_t>(first) * ld;
   const bf16_t *kp = seq + A + kvh * D, *vp = kp + p.kv_heads * D;
 
-  uint32_t voff_k[NL], voff_v[NL];
-  packed_voff<D, KT, 4>(voff_k, wid, lane, ld, false);
-  packed_voff<D, KT, 4>(voff_v, wid, lane, ld, true);
-  auto issue = [&](int t) {
-    const uint32_t buf = lds0 + (t & 1) * 2 * TB;
-    const size_t at = static_cast<size_t>(t) * KT * ld;
-    packed_issue<D, KT, 4>(kp + at, len - t * KT, ld, buf, voff_k, wid);
-    packed_issue<D, KT, 4>(vp + at, len - t * KT, ld, buf + TB, voff_v, wid);
-  };
+  Loads lk, lv;
+  lk.init(kp, len, ld, lds0, wid, lane, false);
+  lv.init(vp, len, ld, lds0 + VB, wid, lane, true);
 
   bf16x8_t qf[H::KS];
   load_row_operand<D>(qf, seq + static_cast<size_t>(q) * ld + h * D, q < len, hf);
@@ -169,105 +227,145 @@ __global__ __launch_bounds__(256, MINB) void packed_fwd_kernel(PackedAttnArgs p)
   f32x16_t acc[H::NF];
 #pragma unroll
   for (int i = 0; i < H::NF; ++i) acc[i] = f32x16_t{};
-  float m = -INFINITY, l = 0.f;
+  float m = -INFINITY, top = -INFINITY, l = 0.f;
   const float c = kLog2e / sqrtf(static_cast<float>(D));
 
-  TileReads<D, false> rd;
-  rd.init(lane, 0, TB);
-  // keys of the workgroup, of the wave, that all of the wave's queries see, and of this lane's query
+  PackedReadsR<D, false> rd;
+  rd.init(lane, lds0);
+  // key tiles of the workgroup and of the wave; the first tile that some query
+  // of the wave does not see whole, and the keys of this lane's query
   const int keys = p.causal ? min(len, row + kPackedRows) : len;
-  const int wave_keys = !active ? 0 : p.causal ? min(len, q0 + 32) : len;
-  const int all_see = p.causal ? q0 + 1 : len;
+  const int wave_keys = q0 >= len ? 0 : p.causal ? min(len, q0 + 32) : len;
+  const int nk = (keys + KT - 1) / KT, nkw = (wave_keys + KT - 1) / KT;
+  const int tmask = (p.causal ? min(len, q0 + 1) : len) / KT;
   const int lim = p.causal ? min(len, q + 1) : len;
-  const int nk = (keys + KT - 1) / KT;
-  issue(0);
-  auto tile = [&](auto stage, int t) {
-    wait_vmcnt<0>();  // this wave's loads of tile t have landed
-    // every wave's loads of tile t have landed, and every wave is done with
-    // tile t - 1, whose buffer the next issue refills
+
+  auto logits = [&](int base, f32x16_t &s) {
+    s = f32x16_t{};
+#pragma unroll
+    for (int kk = 0; kk < H::KS; ++kk) s = mfma32(rd.row(base, 0, kk), qf[kk], s);
+  };
+  auto mask = [&](int t, f32x16_t &s) {
+    const int left = lim - t * KT - hf * 4;
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if ((i >> 2) * 8 + (i & 3) >= left) s[i] = -INFINITY;
+  };
+  // Raw logits are scaled by c > 0, so the scaled maximum is c times the raw
+  // one.  The reference maximum m of a query moves only when a logit exceeds it
+  // by more than kLazyRescale (log2 units; `top` is that in raw logits): O = acc / l
+  // and lse = m + log2 l hold for any m.  ms is the maximum over the half of the
+  // tile's keys that this lane holds, which is enough to see whether any moves.
+  // (Every query sees key 0, so m is finite from tile 0 on.)
+  auto move_max = [&](float ms) {
+    if (__any(ms > top)) {
+      const float mt = max_halves(ms) * c;
+      const float mn = mt > m + kLazyRescale ? mt : m;
+      const float alpha = exp2_hw(m - mn);  // 0 on the first tile (m = -inf), 1 where m stays
+      m = mn;
+      top = (mn + kLazyRescale) / c;
+      l *= alpha;
+#pragma unroll
+      for (int nf = 0; nf < H::NF; ++nf) acc[nf] *= alpha;
+    }
+  };
+
+  f32x16_t s0, s1;
+  lk.template issue<0>();
+  lv.template issue<0>();
+  if (nk > 1) {
+    lk.template issue<TB>();
+    wait_vmcnt<2 * NL>();
+  } else {
+    wait_vmcnt<NL>();
+  }
+  block_barrier();
+  if (nkw > 0) {
+    logits(0, s0);
+    if (tmask <= 0) mask(0, s0);
+    move_max(max16(s0));
+  }
+  auto tile = [&](auto stage, f32x16_t &s, f32x16_t &next, int t) {
+    constexpr int ST = stage.value;
+    wait_vmcnt<0>();  // this wave's loads of V(t) and K(t + 1) have landed
+    // every wave's have, and every wave is done with K(t) and V(t - 1), whose
+    // buffers the next loads refill
     block_barrier();
-    if (t + 1 < nk) issue(t + 1);
-    const lds_char *Ts = smem + stage.value * 2 * TB;
-    const int k0 = t * KT;
-    if (k0 < wave_keys) {  // waves that see none of the tile's keys only load and synchronise
-      constexpr int NS = KT / 32;  // 32-key fragments per tile
-      f32x16_t s[NS];
+    if (t + 2 < nk) lk.template issue<ST * TB>();
+    if (t + 1 < nk) lv.template issue<(1 - ST) * TB>();
+    if (t >= nkw) return;  // waves that see none of the tile's keys only load and synchronise
+    // (past the wave's last tile the logits are of stale data and not used)
+    logits((1 - ST) * TB, next);
+    float l0 = 0.f, l1 = 0.f;
 #pragma unroll
-      for (int f = 0; f < NS; ++f) {
-        s[f] = f32x16_t{};
+    for (int i = 0; i < 16; i += 2) {
+      s[i] = exp2_hw(__builtin_fmaf(s[i], c, -m));
+      s[i + 1] = exp2_hw(__builtin_fmaf(s[i + 1], c, -m));
+      l0 += s[i];
+      l1 += s[i + 1];
+    }
+    l += l0 + l1;
 #pragma unroll
-        for (int kk = 0; kk < H::KS; ++kk) s[f] = mfma32(rd.row(Ts, f, kk), qf[kk], s[f]);
+    for (int st = 0; st < 2; ++st) {
+      const bf16x8_t pb = pack8(s, st);
+#pragma unroll
+      for (int nf = 0; nf < H::NF; ++nf) acc[nf] = mfma32(rd.col(VB + ST * TB, nf, st), pb, acc[nf]);
+    }
+    float ms = max16(next);
+    // The order wanted: the keys' operands, under whose latency the first
+    // exponentials run, then S(t + 1) with the other exponentials and the values'
+    // operands between its products, then P V with the maximum.
+    sched_group<kSchedLds, H::KS>();
+    sched_group<kSchedVector, 20>();
+    sched_group<kSchedTrans, 8>();
+#pragma unroll
+    for (int i = 0; i < H::KS; ++i) {
+      sched_group<kSchedMfma, 1>();
+      sched_group<kSchedVector, 20 / H::KS>();
+      sched_group<kSchedTrans, (8 + H::KS - 1) / H::KS>();
+      sched_group<kSchedLds, (4 * H::NF + H::KS - 1) / H::KS>();
+    }
+#pragma unroll
+    for (int i = 0; i < 2 * H::NF; ++i) {
+      sched_group<kSchedMfma, 1>();
+      sched_group<kSchedVector, 2>();
+    }
+    if (t + 1 < nkw) {
+      if (t + 1 >= tmask) {
+        mask(t + 1, next);
+        ms = max16(next);
       }
-      ColOperands<D, KT, (D <= kPrefetchMaxD), false> vop;  // V^T operands, read under the softmax
-      vop.fetch(Ts, rd);
-      if (k0 + KT > all_see) {
-#pragma unroll
-        for (int f = 0; f < NS; ++f)
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (k0 + f * 32 + (i >> 2) * 8 + hf * 4 + (i & 3) >= lim) s[f][i] = -INFINITY;
-      }
-      // Raw logits are scaled by c > 0, so the scaled maximum is c times the
-      // raw one.  The reference maximum m of a query moves only when its
-      // maximum exceeds m by more than kLazyRescale (log2 units): O = acc / l
-      // and lse = m + log2 l hold for any m.  (Every query sees key 0, so m is
-      // finite after the first tile.)
-      float ms = -INFINITY;
-#pragma unroll
-      for (int f = 0; f < NS; ++f)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) ms = fmaxf(ms, s[f][i]);
-      ms = fmaxf(ms, __shfl_xor(ms, 32, kWave));
-      const float mt = ms * c;
-      const bool grow = mt > m + kLazyRescale;
-      if (__any(grow)) {
-        const float mn = grow ? mt : m;
-        const float alpha = exp2_hw(m - mn);  // 0 on the first tile (m = -inf), 1 where m stays
-        m = mn;
-        l *= alpha;
-#pragma unroll
-        for (int nf = 0; nf < H::NF; ++nf) acc[nf] *= alpha;
-      }
-      float ls = 0.f;
-#pragma unroll
-      for (int f = 0; f < NS; ++f)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float pv = exp2_hw(__builtin_fmaf(s[f][i], c, -m));
-          s[f][i] = pv;
-          ls += pv;
-        }
-      l += ls;
-#pragma unroll
-      for (int st = 0; st < KT / 16; ++st) {
-        const bf16x8_t pb = pack8(s[st >> 1], st & 1);
-#pragma unroll
-        for (int nf = 0; nf < H::NF; ++nf) acc[nf] = mfma32(vop.get(Ts, rd, nf, st), pb, acc[nf]);
-      }
+      move_max(ms);
     }
   };
   for (int t = 0; t < nk; t += 2) {
-    tile(Stage<0>(), t);
-    if (t + 1 < nk) tile(Stage<1>(), t + 1);
+    tile(Stage<0>(), s0, s1, t);
+    if (t + 1 < nk) tile(Stage<1>(), s1, s0, t + 1);
   }
   block_barrier();  // every wave is done with the tile buffers, which the output slots reuse
 
   const float lt = l + __shfl_xor(l, 32, kWave);
   if (q < len && hf == 0) p.lse[static_cast<size_t>(h) * p.tokens + first + q] = (m + log2f(lt)) / kLog2e;
   store_dmajor_lds<D>(p.o + static_cast<size_t>(first + q0) * A + h * D, A, acc, 1.0f / lt, lane,
-                      const_cast<lds_char *>(smem) + wid * 8192, len - q0);
+                      (lds_char *)smem_raw + wid * 8192, len - q0);
 }
 
 // ------------------------------------------------------------------ backward: dQ and D
+//
+// As in the forward a wave runs ahead of itself, here within a tile: dP(t) =
+// V dO^T is in one piece of code with the exponentials of tile t, S(t + 1) with
+// dS(t) = P (dP - D), and dQ^T += K^T dS^T follows.  Three stages of K (tile t
+// for dQ, t + 1 for S, t + 2 in flight) and two of V.
 
-template <int D, int NW, int KT, int MINB>
-__global__ __launch_bounds__(NW * 64, MINB) void packed_bwd_dq_kernel(PackedAttnArgs p) {
+template <int D, int WPE>
+__global__ __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_waves_per_eu(WPE, WPE))) void
+packed_bwd_dq_kernel(PackedAttnArgs p) {
   using H = Head<D>;
-  static_assert(32 * NW == kPackedRows, "one item per workgroup");
-  constexpr int TB = tile_bytes<KT>(), NL = TileLoads<KT, NW>::N, STAGE = 2 * TB;  // K, V
+  constexpr int KT = 32, TB = tile_bytes<KT>(), VB = 3 * TB;  // K, K, K, V, V
+  using Loads = PackedLoads<D, KT, 4>;
+  constexpr int NL = Loads::NL;
   extern __shared__ __attribute__((aligned(1024))) char smem_raw[];
-  const lds_char *smem = (const lds_char *)(smem_raw);
-  const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(smem));
+  const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((const lds_char *)smem_raw));
 
   int item, h, first, len, row;
   packed_item(p.heads, item, h);
@@ -277,20 +375,15 @@ __global__ __launch_bounds__(NW * 64, MINB) void packed_bwd_dq_kernel(PackedAttn
   const int lane = threadIdx.x & 63, hf = lane >> 5;
   const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int q0 = row + wid * 32, q = q0 + (lane & 31);
-  const bool qvalid = q < len, active = q0 < len;
+  const bool qvalid = q < len;
   const bf16_t *seq = p.qkv + static_cast<size_t>(first) * ld;
   const bf16_t *kp = seq + A + kvh * D, *vp = kp + p.kv_heads * D;
   const size_t orow = static_cast<size_t>(first + q) * A + h * D;
   const size_t vec = static_cast<size_t>(h) * p.tokens + first + q;
 
-  uint32_t voff[NL];
-  packed_voff<D, KT, NW>(voff, wid, lane, ld, false);
-  auto issue = [&](int t) {
-    const uint32_t buf = lds0 + (t & 1) * STAGE;
-    const size_t at = static_cast<size_t>(t) * KT * ld;
-    packed_issue<D, KT, NW>(kp + at, len - t * KT, ld, buf, voff, wid);
-    packed_issue<D, KT, NW>(vp + at, len - t * KT, ld, buf + TB, voff, wid);
-  };
+  Loads lk, lv;
+  lk.init(kp, len, ld, lds0, wid, lane, false);
+  lv.init(vp, len, ld, lds0 + VB, wid, lane, false);
 
   bf16x8_t qf[H::KS], df[H::KS];
   load_row_operand<D>(qf, seq + static_cast<size_t>(q) * ld + h * D, qvalid, hf);
@@ -316,62 +409,90 @@ __global__ __launch_bounds__(NW * 64, MINB) void packed_bwd_dq_kernel(PackedAttn
   f32x16_t acc[H::NF];
 #pragma unroll
   for (int i = 0; i < H::NF; ++i) acc[i] = f32x16_t{};
-  constexpr int NS = KT / 32;  // 32-key fragments per tile
   const int keys = p.causal ? min(len, row + kPackedRows) : len;
-  const int wave_keys = !active ? 0 : p.causal ? min(len, q0 + 32) : len;
-  const int all_see = p.causal ? q0 + 1 : len;
+  const int wave_keys = q0 >= len ? 0 : p.causal ? min(len, q0 + 32) : len;
+  const int nk = (keys + KT - 1) / KT, nkw = (wave_keys + KT - 1) / KT;
+  const int tmask = (p.causal ? min(len, q0 + 1) : len) / KT;
   const int lim = p.causal ? min(len, q + 1) : len;
-  const int nk = (keys + KT - 1) / KT;
-  // K: row reads for S^T and the permuted column reads; V (TB further): row reads
-  TileReads<D, true> rd;
-  rd.init(lane, 0, 0);
-  issue(0);
-  auto tile = [&](auto stage, int t) {
-    wait_vmcnt<0>();  // this wave's loads of tile t
-    block_barrier();  // everyone's loads of tile t landed; tile t - 1's buffer is free
-    if (t + 1 < nk) issue(t + 1);
-    const lds_char *Ks = smem + stage.value * STAGE, *Vs = Ks + TB;
-    const int k0 = t * KT;
-    if (k0 < wave_keys) {  // waves that see none of the tile's keys only load and synchronise
-      f32x16_t sv[NS], dp[NS];
+  // K: row reads for S^T and the permuted column reads; V: row reads
+  PackedReadsR<D, true> rd;
+  rd.init(lane, lds0);
+  auto logits = [&](int base, f32x16_t &s) {
+    s = f32x16_t{};
 #pragma unroll
-      for (int f = 0; f < NS; ++f) {
-        sv[f] = f32x16_t{};
-        dp[f] = f32x16_t{};
+    for (int kk = 0; kk < H::KS; ++kk) s = mfma32(rd.row(base, 0, kk), qf[kk], s);
+  };
+
+  // loads in the order K(0), V(0), K(1), then V(t + 1), K(t + 2) in tile t
+  f32x16_t s0, s1;
+  lk.template issue<0>();
+  lv.template issue<0>();
+  if (nk > 1) {
+    lk.template issue<TB>();
+    wait_vmcnt<2 * NL>();
+  } else {
+    wait_vmcnt<NL>();
+  }
+  block_barrier();
+  if (nkw > 0) logits(0, s0);
+  auto tile = [&](auto kstage, auto vstage, f32x16_t &s, f32x16_t &next, int t) {
+    constexpr int KS0 = kstage.value * TB, KS1 = (kstage.value + 1) % 3 * TB, KS2 = (kstage.value + 2) % 3 * TB;
+    constexpr int VS = VB + vstage.value * TB;
+    wait_vmcnt<0>();  // this wave's loads of V(t) and K(t + 1)
+    // everyone's have landed, and everyone is done with K(t - 1) and V(t - 1)
+    block_barrier();
+    if (t + 1 < nk) lv.template issue<(1 - vstage.value) * TB>();
+    if (t + 2 < nk) lk.template issue<KS2>();
+    if (t >= nkw) return;  // waves that see none of the tile's keys only load and synchronise
+    f32x16_t dp{};
 #pragma unroll
-        for (int kk = 0; kk < H::KS; ++kk) {
-          sv[f] = mfma32(rd.row(Ks, f, kk), qf[kk], sv[f]);
-          dp[f] = mfma32(rd.row(Vs, f, kk), df[kk], dp[f]);
-        }
-      }
+    for (int kk = 0; kk < H::KS; ++kk) dp = mfma32(rd.row(VS, 0, kk), df[kk], dp);
 #pragma unroll
-      for (int f = 0; f < NS; ++f)
+    for (int i = 0; i < 16; ++i) s[i] = exp2_hw(__builtin_fmaf(s[i], c, -lse2));
+    // (past the wave's last tile the logits are of stale data and not used)
+    logits(KS1, next);
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          sv[f][i] = exp2_hw(__builtin_fmaf(sv[f][i], c, -lse2)) * (dp[f][i] - dd);  // dS^T
-      if (k0 + KT > all_see) {
-        // register i of fragment f is key k0 + f*32 + 8(i/4) + 4 hf + i%4
+    for (int i = 0; i < 16; ++i) s[i] *= dp[i] - dd;  // dS^T
+    sched_group<kSchedLds, H::KS>();
+    sched_group<kSchedVector, 8>();
+    sched_group<kSchedTrans, 4>();
 #pragma unroll
-        for (int f = 0; f < NS; ++f)
+    for (int i = 0; i < H::KS; ++i) {
+      sched_group<kSchedMfma, 1>();
+      sched_group<kSchedVector, 8 / H::KS>();
+      sched_group<kSchedTrans, (12 + H::KS - 1) / H::KS>();
+      sched_group<kSchedLds, 1>();
+    }
 #pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (k0 + f * 32 + (i >> 2) * 8 + hf * 4 + (i & 3) >= lim) sv[f][i] = 0.f;
-      }
+    for (int i = 0; i < H::KS; ++i) {
+      sched_group<kSchedMfma, 1>();
+      sched_group<kSchedVector, (32 + H::KS - 1) / H::KS>();
+    }
+    if (t >= tmask) {
+      // register i is key t*KT + 8(i/4) + 4 hf + i%4
+      const int left = lim - t * KT - hf * 4;
 #pragma unroll
-      for (int st = 0; st < KT / 16; ++st) {
-        const bf16x8_t sb = pack8(sv[st >> 1], st & 1);
+      for (int i = 0; i < 16; ++i)
+        if ((i >> 2) * 8 + (i & 3) >= left) s[i] = 0.f;
+    }
 #pragma unroll
-        for (int nf = 0; nf < H::NF; ++nf) acc[nf] = mfma32(rd.col(Ks, nf, st), sb, acc[nf]);
-      }
+    for (int st = 0; st < 2; ++st) {
+      const bf16x8_t sb = pack8(s, st);
+#pragma unroll
+      for (int nf = 0; nf < H::NF; ++nf) acc[nf] = mfma32(rd.col(KS0, nf, st), sb, acc[nf]);
     }
   };
-  for (int t = 0; t < nk; t += 2) {
-    tile(Stage<0>(), t);
-    if (t + 1 < nk) tile(Stage<1>(), t + 1);
+  for (int t = 0; t < nk; t += 6) {
+    tile(Stage<0>(), Stage<0>(), s0, s1, t);
+    if (t + 1 < nk) tile(Stage<1>(), Stage<1>(), s1, s0, t + 1);
+    if (t + 2 < nk) tile(Stage<2>(), Stage<0>(), s0, s1, t + 2);
+    if (t + 3 < nk) tile(Stage<0>(), Stage<1>(), s1, s0, t + 3);
+    if (t + 4 < nk) tile(Stage<1>(), Stage<0>(), s0, s1, t + 4);
+    if (t + 5 < nk) tile(Stage<2>(), Stage<1>(), s1, s0, t + 5);
   }
   block_barrier();  // the output slots reuse the tile buffers
   store_dmajor_lds<D>(p.dqkv + static_cast<size_t>(first + q0) * ld + h * D, ld, acc,
-                      1.0f / sqrtf(static_cast<float>(D)), lane, const_cast<lds_char *>(smem) + wid * 8192, len - q0);
+                      1.0f / sqrtf(static_cast<float>(D)), lane, (lds_char *)smem_raw + wid * 8192, len - q0);
 }
 
 // ------------------------------------------------------------------ backward: dK, dV
@@ -394,11 +515,12 @@ constexpr int packed_dkdv_stage() {
 constexpr bool dkdv_v_in_lds(int d) { return d > 80; }
 
 template <int D, int NW, int KT, int MINB>
-__global__ __launch_bounds__(NW * 64, MINB) void packed_bwd_dkdv_kernel(PackedAttnArgs p) {
+__global__ __attribute__((amdgpu_flat_work_group_size(NW * 64, NW * 64), amdgpu_waves_per_eu(MINB, MINB))) void packed_bwd_dkdv_kernel(PackedAttnArgs p) {
   using H = Head<D>;
   static_assert(32 * NW == kPackedRows, "one item per workgroup");
-  constexpr int TB = tile_bytes<KT>(), NL = TileLoads<KT, NW>::N, TILES = 2 * TB;  // Q, dO
+  constexpr int TB = tile_bytes<KT>(), TILES = 2 * TB;  // Q, dO
   constexpr int STAGE = packed_dkdv_stage<KT>(), NS = KT / 32;
+  using Loads = PackedLoads<D, KT, NW>;
   constexpr bool VL = dkdv_v_in_lds(D);
   extern __shared__ __attribute__((aligned(1024))) char smem_raw[];
   const lds_char *smem = (const lds_char *)(smem_raw);
@@ -417,38 +539,33 @@ __global__ __launch_bounds__(NW * 64, MINB) void packed_bwd_dkdv_kernel(PackedAt
   const bf16_t *seq = p.qkv + static_cast<size_t>(first) * ld;
   const bf16_t *dseq = p.dO + static_cast<size_t>(first) * A;
 
-  // Two loads per tile and wave, the second four rows further, where the swizzle
-  // swaps neighbouring chunks: its offset is made from the first one's when it
-  // is needed (rows are multiples of 32 bytes).
-  static_assert(NL == 2, "two loads per tile and wave");
-  uint32_t v0[NL];
-  packed_voff<D, KT, NW>(v0, wid, lane, ld, false);
-  const uint32_t vq = v0[0];
-  packed_voff<D, KT, NW>(v0, wid, lane, A, false);
-  const uint32_t vd = v0[0];
-  auto load2 = [&](const bf16_t *src, int rows, int rld, uint32_t lds_tile, uint32_t v) {
-    const uint32_t both[2] = {v, (v ^ 16) + static_cast<uint32_t>(8 * rld)};
-    packed_issue<D, KT, NW>(src, rows, rld, lds_tile, both, wid);
-  };
   // query tiles t0 .. nq - 1 of each of the group's heads in turn
   const int t0 = p.causal ? row / KT : 0, nq = (len + KT - 1) / KT;
   const int total = (nq - t0) * group;
   int ih = kvh * group, it = t0;  // head and tile issued next
-  auto issue = [&](int n) {
-    const uint32_t buf = lds0 + (n & 1) * STAGE;
-    const int rem = len - it * KT;
-    load2(seq + static_cast<size_t>(it) * KT * ld + ih * D, rem, ld, buf, vq);
-    load2(dseq + static_cast<size_t>(it) * KT * A + ih * D, rem, A, buf + TB, vd);
-    // the tile's vectors; past the sequence they read as zero, as Q and dO do:
-    // P = 1 then meets zeros only
-    const size_t vec = static_cast<size_t>(ih) * p.tokens + first + it * KT;
-    const uint32_t ext = static_cast<uint32_t>(min(rem, KT)) * 4;
-    if (wid == 0)
-      buffer_load_lds4(make_rsrc(p.nlse + vec, ext), __builtin_amdgcn_readfirstlane(buf + TILES), lane * 4, 0);
-    if (wid == 1)
-      buffer_load_lds4(make_rsrc(p.ndvec + vec, ext), __builtin_amdgcn_readfirstlane(buf + TILES + 64 * 4), lane * 4,
-                       0);
-    if (++it == nq) it = t0, ++ih;
+  Loads lq, ld_o;
+  lq.init(seq + static_cast<size_t>(t0) * KT * ld + ih * D, len - t0 * KT, ld, lds0, wid, lane, false);
+  ld_o.init(dseq + static_cast<size_t>(t0) * KT * A + ih * D, len - t0 * KT, A, lds0 + TB, wid, lane, false);
+  // wave 0 loads the tile's -lse sqrt(D), wave 1 its -D_i; past the sequence
+  // they read as zero, as Q and dO do: P = 1 then meets zeros only
+  const float *vecs = (wid == 0 ? p.nlse : p.ndvec) + first + t0 * KT;
+  const uint32_t vec_lds = __builtin_amdgcn_readfirstlane(lds0 + TILES + (wid == 0 ? 0 : 256));
+  const uint32_t vec_bytes = static_cast<uint32_t>(len - t0 * KT) * 4;
+  u32x4_t rvec = make_rsrc(vecs + static_cast<size_t>(ih) * p.tokens, vec_bytes);
+  uint32_t vec_off = 0;
+  auto issue = [&](auto stage) {
+    constexpr int ST = decltype(stage)::value * STAGE;
+    lq.template issue<ST>();
+    ld_o.template issue<ST>();
+    if (wid < 2) issue_lds4<ST>(rvec, vec_lds, lane * 4, vec_off);
+    vec_off += KT * 4;
+    if (++it == nq) {
+      it = t0, ++ih;
+      lq.start(seq + static_cast<size_t>(t0) * KT * ld + ih * D, len - t0 * KT, ld);
+      ld_o.start(dseq + static_cast<size_t>(t0) * KT * A + ih * D, len - t0 * KT, A);
+      rvec = make_rsrc(vecs + static_cast<size_t>(ih) * p.tokens, vec_bytes);
+      vec_off = 0;
+    }
   };
 
   bf16x8_t kf[H::KS], vf[H::KS];
@@ -469,7 +586,7 @@ __global__ __launch_bounds__(NW * 64, MINB) void packed_bwd_dkdv_kernel(PackedAt
   const float c = kLog2e / sqrtf(static_cast<float>(D));
   PackedReads<D, true> rd;
   rd.init(lane, lds0);
-  issue(0);
+  issue(Stage<0>());
   int ct = t0;  // the tile computed next
   auto tile = [&](auto stage, int n) {
     constexpr int ST = stage.value * STAGE;
@@ -477,7 +594,7 @@ __global__ __launch_bounds__(NW * 64, MINB) void packed_bwd_dkdv_kernel(PackedAt
     // every wave's loads of tile n have landed, and every wave is done with
     // tile n - 1, whose buffer is refilled next
     block_barrier();
-    if (n + 1 < total) issue(n + 1);
+    if (n + 1 < total) issue(Stage<1 - stage.value>());
     const int q0 = ct * KT;
     if (++ct == nq) ct = t0;
     // waves whose keys all lie past the sequence, or (causal) behind every
@@ -539,34 +656,21 @@ __global__ __launch_bounds__(NW * 64, MINB) void packed_bwd_dkdv_kernel(PackedAt
 
 // Launch shapes: 4 waves of 32 queries (forward, dQ) or keys (dK/dV); KT is the
 // token tile streamed through LDS, MINB the workgroups each CU must hold at once.
-constexpr int kFwdKT = 32, kFwdMinBlocks = 3, kFwdSmallGrid = 256;
-constexpr int kDqWaves = 4, kDqKT = 32, kDqMinBlocks = 2;
 constexpr int kDkvWaves = 4, kDkvKT = 32, kDkvMinBlocks = 2;
 
-template <int D, int KT, int MINB>
-void launch_fwd_cfg(const PackedAttnArgs &a, hipStream_t s) {
-  // two stages of (K, V) tiles; the per-wave 8 KB output slots reuse them
-  constexpr int lds = std::max(4 * tile_bytes<KT>(), 4 * 8192);
-  hipLaunchKernelGGL((packed_fwd_kernel<D, KT, MINB>), dim3(a.slots * a.heads), dim3(256), lds, s, a);
-}
-
-// A grid that leaves CUs idle runs each workgroup's tiles back to back with
-// nothing else on the CU to hide their latency: there fewer, longer tiles win.
 template <int D>
 void launch_fwd_d(const PackedAttnArgs &a, hipStream_t s) {
-  if (static_cast<long>(a.slots) * a.heads <= kFwdSmallGrid)
-    launch_fwd_cfg<D, 64, 2>(a, s);
-  else
-    launch_fwd_cfg<D, kFwdKT, kFwdMinBlocks>(a, s);
+  // the stages of K and V tiles; the per-wave 8 KB output slots reuse them
+  constexpr int lds = std::max(4 * tile_bytes<32>(), 4 * 8192), waves = D == 64 ? 4 : D == 80 ? 3 : 2;
+  hipLaunchKernelGGL((packed_fwd_kernel<D, waves>), dim3(a.slots * a.heads), dim3(256), lds, s, a);
 }
 
 template <int D>
 void launch_bwd_d(const PackedAttnArgs &a, hipStream_t s) {
-  constexpr int kDqLds = std::max(4 * tile_bytes<kDqKT>(), kDqWaves * 8192);
+  constexpr int kDqLds = std::max(5 * tile_bytes<32>(), 4 * 8192), waves = D == 64 ? 3 : 2;
   constexpr int kDkvLds =
       std::max(2 * packed_dkdv_stage<kDkvKT>() + (dkdv_v_in_lds(D) ? kDkvWaves * 32 * D * 2 : 0), kDkvWaves * 8192);
-  hipLaunchKernelGGL((packed_bwd_dq_kernel<D, kDqWaves, kDqKT, kDqMinBlocks>), dim3(a.slots * a.heads),
-                     dim3(kDqWaves * 64), kDqLds, s, a);
+  hipLaunchKernelGGL((packed_bwd_dq_kernel<D, waves>), dim3(a.slots * a.heads), dim3(256), kDqLds, s, a);
   hipLaunchKernelGGL((packed_bwd_dkdv_kernel<D, kDkvWaves, kDkvKT, kDkvMinBlocks>), dim3(a.slots * a.kv_heads),
                      dim3(kDkvWaves * 64), kDkvLds, s, a);
 }

@@ -775,32 +775,6 @@ bool launch_any(const GemmArgs &a, hipStream_t s) {
 // 537 -> 520, 410 -> 397.
 // ---------------------------------------------------------------------------
 
-// One 1 KB wave load straight to LDS at base + OFF + 16 * lane.  M0 (the LDS
-// address) is left set: nothing else here reads it without setting it.
-template <int OFF>
-__device__ __forceinline__ void issue_lds16(const u32x4_t &rsrc, uint32_t base, uint32_t voff, uint32_t soff) {
-  asm volatile(
-      "s_add_u32 m0, %0, %4\n\t"
-      "s_nop 0\n\t"
-      "buffer_load_dwordx4 %1, %2, %3 offen lds"
-      :
-      : "s"(base), "v"(voff), "s"(rsrc), "s"(soff), "i"(OFF)
-      : "memory", "scc");
-}
-// The same for the lanes of `mask` only.
-template <int OFF>
-__device__ __forceinline__ void issue_lds16(const u32x4_t &rsrc, uint32_t base, uint32_t voff, uint32_t soff,
-                                            uint64_t mask) {
-  asm volatile(
-      "s_add_u32 m0, %0, %4\n\t"
-      "s_mov_b64 exec, %5\n\t"
-      "buffer_load_dwordx4 %1, %2, %3 offen lds\n\t"
-      "s_mov_b64 exec, -1"
-      :
-      : "s"(base), "v"(voff), "s"(rsrc), "s"(soff), "i"(OFF), "s"(mask)
-      : "memory", "scc");
-}
-
 // One operand's half tiles: NWV waves of 2 * FH fragments of 16 rows each;
 // half h holds each wave's fragments [h * FH, (h + 1) * FH).
 template <int NWV, int FH, bool TRANS>

@@ -37,6 +37,45 @@ __device__ __forceinline__ void buffer_load_lds16(const u32x4_t &rsrc, uint32_t 
       : "memory");
 }
 
+// One 1 KB wave load straight to LDS at base + OFF + 16 * lane.  M0 (the LDS
+// address) is left set: nothing else here reads it without setting it.
+template <int OFF>
+__device__ __forceinline__ void issue_lds16(const u32x4_t &rsrc, uint32_t base, uint32_t voff, uint32_t soff) {
+  asm volatile(
+      "s_add_u32 m0, %0, %4\n\t"
+      "s_nop 0\n\t"
+      "buffer_load_dwordx4 %1, %2, %3 offen lds"
+      :
+      : "s"(base), "v"(voff), "s"(rsrc), "s"(soff), "i"(OFF)
+      : "memory", "scc");
+}
+
+// The same for the lanes of `mask` only.
+template <int OFF>
+__device__ __forceinline__ void issue_lds16(const u32x4_t &rsrc, uint32_t base, uint32_t voff, uint32_t soff,
+                                            uint64_t mask) {
+  asm volatile(
+      "s_add_u32 m0, %0, %4\n\t"
+      "s_mov_b64 exec, %5\n\t"
+      "buffer_load_dwordx4 %1, %2, %3 offen lds\n\t"
+      "s_mov_b64 exec, -1"
+      :
+      : "s"(base), "v"(voff), "s"(rsrc), "s"(soff), "i"(OFF), "s"(mask)
+      : "memory", "scc");
+}
+
+// The 4-byte-per-lane form of issue_lds16: base + OFF + 4 * lane.
+template <int OFF>
+__device__ __forceinline__ void issue_lds4(const u32x4_t &rsrc, uint32_t base, uint32_t voff, uint32_t soff) {
+  asm volatile(
+      "s_add_u32 m0, %0, %4\n\t"
+      "s_nop 0\n\t"
+      "buffer_load_dword %1, %2, %3 offen lds"
+      :
+      : "s"(base), "v"(voff), "s"(rsrc), "s"(soff), "i"(OFF)
+      : "memory", "scc");
+}
+
 // The 4-byte-per-lane form: writes lds_addr + 4 * lane.
 __device__ __forceinline__ void buffer_load_lds4(const u32x4_t &rsrc, uint32_t lds_addr, uint32_t voff,
                                                  uint32_t soff) {
