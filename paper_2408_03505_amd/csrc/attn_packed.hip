@@ -52,10 +52,8 @@ __device__ __forceinline__ void packed_item(int heads, int &item, int &h) {
 }
 
 // The item's sequence and first row in it, kept inside the tensors whatever
-// the list holds; false past the list's end.
-__device__ __forceinline__ bool load_item(const PackedPlan *plan, int slots, int tokens, int i, int &first, int &len,
-                                          int &row) {
-  if (i >= min(plan->count, slots)) return false;
+// the list holds; false for the empty items behind the list's end.
+__device__ __forceinline__ bool load_item(const PackedPlan *plan, int tokens, int i, int &first, int &len, int &row) {
   const PackedItem it = plan->item[i];
   first = __builtin_amdgcn_readfirstlane(min(max(it.first, 0), tokens));
   len = __builtin_amdgcn_readfirstlane(min(max(it.len, 0), tokens - first));
@@ -207,7 +205,7 @@ packed_fwd_kernel(PackedAttnArgs p) {
 
   int item, h, first, len, row;
   packed_item(p.heads, item, h);
-  if (!load_item(p.plan, p.slots, p.tokens, item, first, len, row)) return;
+  if (!load_item(p.plan, p.tokens, item, first, len, row)) return;
   const int kvh = h / (p.heads / p.kv_heads);
   const int A = p.heads * D, ld = A + 2 * p.kv_heads * D;
   const int lane = threadIdx.x & 63, hf = lane >> 5;
@@ -369,7 +367,7 @@ packed_bwd_dq_kernel(PackedAttnArgs p) {
 
   int item, h, first, len, row;
   packed_item(p.heads, item, h);
-  if (!load_item(p.plan, p.slots, p.tokens, item, first, len, row)) return;
+  if (!load_item(p.plan, p.tokens, item, first, len, row)) return;
   const int kvh = h / (p.heads / p.kv_heads);
   const int A = p.heads * D, ld = A + 2 * p.kv_heads * D;
   const int lane = threadIdx.x & 63, hf = lane >> 5;
@@ -528,7 +526,7 @@ __global__ __attribute__((amdgpu_flat_work_group_size(NW * 64, NW * 64), amdgpu_
 
   int item, kvh, first, len, row;
   packed_item(p.kv_heads, item, kvh);
-  if (!load_item(p.plan, p.slots, p.tokens, item, first, len, row)) return;
+  if (!load_item(p.plan, p.tokens, item, first, len, row)) return;
   const int group = p.heads / p.kv_heads;
   const int A = p.heads * D, ld = A + 2 * p.kv_heads * D;
   const int lane = threadIdx.x & 63, hf = lane >> 5;
@@ -667,7 +665,7 @@ void launch_fwd_d(const PackedAttnArgs &a, hipStream_t s) {
 
 template <int D>
 void launch_bwd_d(const PackedAttnArgs &a, hipStream_t s) {
-  constexpr int kDqLds = std::max(5 * tile_bytes<32>(), 4 * 8192), waves = D == 64 ? 3 : 2;
+  constexpr int kDqLds = std::max(5 * tile_bytes<32>(), 4 * 8192), waves = D == 128 ? 2 : 3;
   constexpr int kDkvLds =
       std::max(2 * packed_dkdv_stage<kDkvKT>() + (dkdv_v_in_lds(D) ? kDkvWaves * 32 * D * 2 : 0), kDkvWaves * 8192);
   hipLaunchKernelGGL((packed_bwd_dq_kernel<D, waves>), dim3(a.slots * a.heads), dim3(256), kDqLds, s, a);

@@ -55,7 +55,8 @@ inline size_t attn_bwd_ws_bytes(int B, int S, int heads) {
 
 // ---- Packed sequences: the work list that packed attention reads.  One item
 // per kPackedRows tokens of a sequence; a batch of `tokens` rows in `seqs`
-// sequences has at most packed_slots of them.
+// sequences has at most packed_slots of them, and the slots behind the list's
+// end hold empty items.
 constexpr int kPackedRows = 128;
 
 struct PackedItem {

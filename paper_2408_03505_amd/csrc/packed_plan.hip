@@ -25,7 +25,7 @@ __device__ __forceinline__ int tiles_of(int len) { return (len + kPackedRows - 1
 
 __global__ __launch_bounds__(256) void packed_plan_kernel(int tokens, int seqs, int cap, const int *__restrict__ cu,
                                                           PackedPlan *__restrict__ plan) {
-  __shared__ int tiles[256], first_item[256], firsts[256], lens[256];
+  __shared__ int tiles[256];
   const int tid = threadIdx.x, mine = blockIdx.x * 256 + tid;
   int first = 0, len = 0;
   if (mine < seqs) sequence(cu, mine, tokens, first, len);
@@ -37,25 +37,24 @@ __global__ __launch_bounds__(256) void packed_plan_kernel(int tokens, int seqs, 
     __syncthreads();
     tiles[tid] = tiles_of(l);
     __syncthreads();
-    const int n = min(256, seqs - j0);
-    for (int j = 0; j < n; ++j) {
-      const int o = tiles[j];
-      total += o;
-      if (o > t || (o == t && j0 + j < mine)) before += o;
-    }
+    const int n = min(256, seqs - j0);  // (the others of the 256 have no tiles)
+    for (int j = 0; j < n; j += 8)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int o = tiles[j + e];
+        total += o;
+        if (o > t || (o == t && j0 + j + e < mine)) before += o;
+      }
   }
-  // (offsets that go backwards could ask for more items than there is room for)
-  first_item[tid] = static_cast<int>(min(before, static_cast<long>(cap)));
-  firsts[tid] = first;
-  lens[tid] = len;
-  __syncthreads();
-  for (int j = 0; j < min(256, seqs - static_cast<int>(blockIdx.x) * 256); ++j) {
-    const int nt = tiles_of(lens[j]);
-    for (int k = tid; k < nt && first_item[j] + k < cap; k += 256)
-      // the last tile first: with causal attention it is the longest
-      plan->item[first_item[j] + k] = PackedItem{firsts[j], lens[j], (nt - 1 - k) * kPackedRows, 0};
+  // the last tile first: with causal attention it is the longest (offsets that
+  // go backwards could ask for more items than there is room for)
+  for (int k = 0; k < t && before + k < cap; ++k)
+    plan->item[before + k] = PackedItem{first, len, (t - 1 - k) * kPackedRows, 0};
+  // empty items behind the list's end
+  if (blockIdx.x == 0) {
+    for (long k = total + tid; k < cap; k += 256) plan->item[k] = PackedItem{0, 0, 0, 0};
+    if (tid == 0) plan->count = static_cast<int>(min(total, static_cast<long>(cap)));
   }
-  if (mine == 0) plan->count = static_cast<int>(min(total, static_cast<long>(cap)));
 }
 
 }  // namespace
