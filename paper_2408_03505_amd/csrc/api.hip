@@ -318,6 +318,16 @@ bool glu_dgrad(int M, int F, int H, int act, const bf16_t *dout, const bf16_t *W
   return launch_gemm_dgrad(a, Epi::kGluGrad, ws, ws_bytes, s);
 }
 
+// dY[M, H] = dgu[M, 2F] Wgu[2F, H]
+bool glu_up_dgrad(int M, int F, int H, const bf16_t *dgu, const bf16_t *W, bf16_t *dY, void *ws, size_t ws_bytes,
+                  hipStream_t s) {
+  GemmArgs a{};
+  a.M = M, a.N = H, a.K = 2 * F;
+  a.A = dgu, a.lda = 2 * F, a.B = W, a.ldb = H;
+  a.Y = dY, a.ldy = H;
+  return launch_gemm_dgrad(a, Epi::kPlainTail, ws, ws_bytes, s);
+}
+
 int linear_dims(const char *fn, int M, std::initializer_list<int> feats) {
   int r = check_dims(fn, {M});
   if (r) return r;
@@ -1141,8 +1151,7 @@ int enc_glu_up_bwd_data(int M, int H, int F, const enc_bf16 *dgu, const enc_bf16
   c.req(dgu, "dgu").req(w_gu, "w_gu").req(dy2, "dy2");
   if (c.code) return c.code;
   if ((r = check_gemm_ws(fn, ws, ws_bytes, M, H, 2 * F))) return r;
-  if (!gemm_dgrad(M, 2 * F, H, dgu, w_gu, nullptr, dy2, ws, ws_bytes, as_stream(stream)))
-    return refused_after_checks(fn);
+  if (!glu_up_dgrad(M, F, H, dgu, w_gu, dy2, ws, ws_bytes, as_stream(stream))) return refused_after_checks(fn);
   return launched(fn);
 }
 

@@ -126,6 +126,18 @@ __device__ __forceinline__ void glu_grad_store8(const float (&dh)[8], u32x4_t gw
   stg16_nt(du, w);
 }
 
+// Whether an epilogue evaluates an activation (those products have rows of the
+// cost table of their own).
+constexpr bool has_activation(Epi e) {
+  return e == Epi::kBiasGelu || e == Epi::kGeluGrad || e == Epi::kGlu || e == Epi::kGluGrad;
+}
+
+// Whether the direct-to-LDS kernels of an epilogue end a contraction inside a
+// 64-wide k-step.  The gated feed-forward block's do: its width is a fraction of
+// the model's (8/3, say), often no multiple of 64.  (The others keep the
+// register-staged kernel there, and with it their results.)
+constexpr bool takes_tail(Epi e) { return e == Epi::kGlu || e == Epi::kGluGrad || e == Epi::kPlainTail; }
+
 // Logical tile for this workgroup.  MI355X dispatches workgroup i to XCD
 // i % 8.  When the tile grid splits evenly, the XCDs form two halves along M,
 // the four XCDs of a half split its column tiles, and each XCD walks its block
@@ -775,6 +787,9 @@ bool launch_any(const GemmArgs &a, hipStream_t s) {
 // 537 -> 520, 410 -> 397.
 // ---------------------------------------------------------------------------
 
+// A buffer offset past the end of every operand: such a load returns zero.
+constexpr uint32_t kPastEnd = 0xfffffff0u;
+
 // One operand's half tiles: NWV waves of 2 * FH fragments of 16 rows each;
 // half h holds each wave's fragments [h * FH, (h + 1) * FH).
 template <int NWV, int FH, bool TRANS>
@@ -840,6 +855,19 @@ struct HalfTile {
     // slots from the other group's MFMAs
 #pragma unroll
     for (int i = 0; i < NOFF; ++i) asm volatile("" : "+v"(off[i]));
+  }
+  // From here on the columns from `cols` of a k-step on read as zero: the last
+  // k-step of a contraction that is no multiple of 64 (a strided operand ends
+  // with its last row).
+  __device__ __forceinline__ void end_columns(int cols, int wid, int lane) {
+    if constexpr (!TRANS) {
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        using T = NtTile<BK>;
+        const int o = wid * WB + i * 1024 + lane * 16;
+        if (((((o % T::RB) >> 4) ^ ((o / T::RB / T::RP) % T::CPR)) * 8) >= cols) voff[i] = kPastEnd;
+      }
+    }
   }
   template <int OFF>
   __device__ __forceinline__ void issue(uint32_t wbase, uint32_t soff) const {
@@ -928,11 +956,14 @@ __global__ __launch_bounds__(512, 1) void gemm_half_kernel(GemmArgs p, uint32_t 
   const int nk = (klen + BK - 1) / BK;
   constexpr std::integral_constant<int, 0> c0{};
   constexpr std::integral_constant<int, 1> c1{};
+  constexpr bool TAIL = takes_tail(EPI);
+  // (with the branches of TAIL the compiler loses track of the offsets' being scalar)
+  auto scalar = [](uint32_t v) { return TAIL ? __builtin_amdgcn_readfirstlane(v) : v; };
   auto issue_a = [&](auto st, auto h) {
-    la.template issue<(st.value * 2 + h.value) * TA::BYTES>(wa, so_a + (h.value ? la.half_off : 0u));
+    la.template issue<(st.value * 2 + h.value) * TA::BYTES>(wa, scalar(so_a + (h.value ? la.half_off : 0u)));
   };
   auto issue_b = [&](auto st, auto h) {
-    lb.template issue<(st.value * 2 + h.value) * TB::BYTES>(wb, so_b + (h.value ? lb.half_off : 0u));
+    lb.template issue<(st.value * 2 + h.value) * TB::BYTES>(wb, scalar(so_b + (h.value ? lb.half_off : 0u)));
   };
   auto barrier = [] {
     __builtin_amdgcn_sched_barrier(0);
@@ -990,8 +1021,16 @@ __global__ __launch_bounds__(512, 1) void gemm_half_kernel(GemmArgs p, uint32_t 
     }
   };
 
+  // a contraction that is no multiple of 64 (not split): the last k-step's columns
+  const int tail = TAIL ? p.K % BK : 0;
+  auto end_columns = [&] {
+    la.end_columns(tail, wid, lane);
+    lb.end_columns(tail, wid, lane);
+  };
+
   // k-steps 0 and 1, in the order the loop reads them (X of step 0 is B0, of
   // step 1 B1)
+  if (TAIL && tail && nk == 1) end_columns();
   issue_b(c0, c0);
   issue_a(c0, c0);
   issue_b(c0, c1);
@@ -999,6 +1038,7 @@ __global__ __launch_bounds__(512, 1) void gemm_half_kernel(GemmArgs p, uint32_t 
   so_a += a_step;
   so_b += b_step;
   if (nk > 1) {
+    if (TAIL && tail && nk == 2) end_columns();
     issue_b(c1, c1);
     issue_a(c1, c0);
     issue_b(c1, c0);
@@ -1035,6 +1075,7 @@ __global__ __launch_bounds__(512, 1) void gemm_half_kernel(GemmArgs p, uint32_t 
     // ---- L0, M0
     if (more1) issue_a(Y, c1);
     so_a += a_step;
+    if (TAIL && !FULL && tail && t + 3 == nk) end_columns();  // the loads left are the last k-step's
     read_a(st, c0);
     wait3(more2, more1, cnt<3 * NA + 2 * NB - PA>(), cnt<3 * NA + 2 * NB - PA>(), cnt<NA - PA>());
     barrier();
@@ -1067,7 +1108,7 @@ __global__ __launch_bounds__(512, 1) void gemm_half_kernel(GemmArgs p, uint32_t 
   };
   auto k_loop = [&](auto db) {
     int t = 0;
-    for (; t + 3 < nk; t += 2) {
+    for (; t + 3 < nk - (tail ? 1 : 0); t += 2) {
       step(c0, c1, db, t);
       step(c1, c1, db, t + 1);
     }
@@ -1191,6 +1232,17 @@ struct RingTile {
       for (int i = 0; i < NOFF; ++i) asm volatile("" : "+v"(off[g][i]));
     }
   }
+  // As HalfTile's.
+  __device__ __forceinline__ void end_columns(int cols, int wid, int lane) {
+    if constexpr (!TRANS) {
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        using T = NtTile<BK>;
+        const int o = wid * WB + i * 1024 + lane * 16;
+        if (((((o % T::RB) >> 4) ^ ((o / T::RB / T::RP) % T::CPR)) * 8) >= cols) voff[i] = kPastEnd;
+      }
+    }
+  }
   template <int OFF, int I = 0>
   __device__ __forceinline__ void issue(uint32_t wbase, uint32_t soff) const {
     if constexpr (I < NI) {
@@ -1279,7 +1331,16 @@ __global__ __launch_bounds__(512, 2 * WGS) void gemm_ring_kernel(GemmArgs p, uin
   const int nk = (klen + BK - 1) / BK;
   constexpr std::integral_constant<int, 0> c0{};
   constexpr std::integral_constant<int, 1> c1{};
-  auto issue = [&](auto st) {
+  constexpr bool TAIL = takes_tail(EPI);
+  const int tail = TAIL ? p.K % BK : 0;  // a contraction that is no multiple of 64 (not split)
+  // loads of k-step k; LAST: it may be the last one
+  auto issue = [&](auto st, auto last, int k) {
+    if constexpr (TAIL && decltype(last)::value) {
+      if (tail && k == nk - 1) {
+        la.end_columns(tail, wid, lane);
+        lb.end_columns(tail, wid, lane);
+      }
+    }
     la.template issue<st.value * TA::BYTES>(wa, so_a);
     lb.template issue<st.value * TB::BYTES>(wb, so_b);
     so_a += a_step;
@@ -1304,7 +1365,7 @@ __global__ __launch_bounds__(512, 2 * WGS) void gemm_ring_kernel(GemmArgs p, uin
         wait_ksteps<PS, D - 1>(min(t + D - 1, nk - 1) - t);
       barrier();
     }
-    if (FULL || t + D < nk) issue(cnt<(ST + D) % S>());
+    if (FULL || t + D < nk) issue(cnt<(ST + D) % S>(), cnt<!FULL>(), t + D);
 #pragma unroll
     for (int kk = 0; kk < KS; ++kk) {
 #pragma unroll
@@ -1345,7 +1406,7 @@ __global__ __launch_bounds__(512, 2 * WGS) void gemm_ring_kernel(GemmArgs p, uin
   };
 
   // the first D k-steps
-  with_counts([&](auto... i) { ((i.value < nk ? issue(i) : void()), ...); }, std::make_integer_sequence<int, D>{});
+  with_counts([&](auto... i) { ((i.value < nk ? issue(i, c1, i.value) : void()), ...); }, std::make_integer_sequence<int, D>{});
   if constexpr (STAG) {
     wait_ksteps<PS, D - 1>(min(D, nk) - 1);
     barrier();
@@ -1354,7 +1415,7 @@ __global__ __launch_bounds__(512, 2 * WGS) void gemm_ring_kernel(GemmArgs p, uin
 
   auto k_loop = [&](auto db) {
     int t = 0;
-    for (; t + S - 1 + D < nk; t += S)
+    for (; t + S - 1 + D < nk - (tail ? 1 : 0); t += S)
       with_counts([&](auto... i) { (step(i, c1, db, t + i.value), ...); }, std::make_integer_sequence<int, S>{});
     while (t < nk)
       with_counts([&](auto... i) { ((t < nk ? (step(i, c0, db, t), void(++t)) : void()), ...); },
@@ -1399,12 +1460,6 @@ bool launch_ring_cfg(const GemmArgs &a, uint32_t a_bytes, uint32_t b_bytes, hipS
   return true;
 }
 
-// Whether an epilogue evaluates an activation (those products have rows of the
-// cost table of their own).
-constexpr bool has_activation(Epi e) {
-  return e == Epi::kBiasGelu || e == Epi::kGeluGrad || e == Epi::kGlu || e == Epi::kGluGrad;
-}
-
 // Direct-to-LDS path on tile t (of kTiles): 256-row tiles run gemm_half_kernel,
 // the others gemm_ring_kernel.
 // Returns false when the operands do not fit the path's constraints.  Only the
@@ -1414,7 +1469,7 @@ template <bool AT, bool BT, Epi EPI>
 bool launch_lds(const GemmArgs &a, hipStream_t s, TileShape t) {
   constexpr bool gelu = has_activation(EPI);
   constexpr GemmLayout row = !AT && EPI == Epi::kF32 ? kSplit : gemm_layout(AT, BT, gelu);
-  if (!lds_fits(a.M, a.N, a.K, a.lda, a.ldb, AT, BT)) return false;
+  if (!lds_fits(a.M, a.N, a.K, a.lda, a.ldb, AT, BT, takes_tail(EPI))) return false;
   // operand extents (bytes) bound the buffer loads
   const uint32_t ab = static_cast<uint32_t>(static_cast<uint64_t>(AT ? a.K : a.M) * a.lda * 2);
   const uint32_t bb = static_cast<uint32_t>(static_cast<uint64_t>(BT ? a.K : a.N) * a.ldb * 2);
@@ -1625,6 +1680,10 @@ bool launch_gemm_dgrad(const GemmArgs &a, Epi epi, void *ws, size_t ws_bytes, hi
     case Epi::kGeluGrad: return dgrad_any<Epi::kGeluGrad>(a, ws, ws_bytes, s);
     case Epi::kResid: return dgrad_any<Epi::kResid>(a, ws, ws_bytes, s);
     case Epi::kGluGrad: return dgrad_any<Epi::kGluGrad>(a, ws, ws_bytes, s);
+    case Epi::kPlainTail:
+      // (a contraction of whole k-steps is the plain product, split or not)
+      return (a.K % 64 != 0 && launch_lds<false, true, Epi::kPlainTail>(a, s)) ||
+             dgrad_any<Epi::kPlain>(a, ws, ws_bytes, s);
     default: return false;
   }
 }

@@ -281,11 +281,12 @@ inline SplitPlan gemm_split_plan(int M, int N, int K) {
 
 // Whether the direct-to-LDS kernels take a product (operands A(m, k) and
 // B(n, k) with leading dimensions lda, ldb; AT / BT: stored k-major):
-// contiguous-k operands need whole 64-wide k-steps, and the operand extents
-// that bound the buffer loads keep every offset below 2^32.  The others run
-// the register-staged kernel.
-inline bool lds_fits(int M, int N, int K, int lda, int ldb, bool AT, bool BT) {
-  if ((!AT || !BT) && K % 64 != 0) return false;
+// contiguous-k operands need whole 64-wide k-steps (unless the kernel ends the
+// last one where the contraction does: tail), and the operand extents that bound
+// the buffer loads keep every offset below 2^32.  The others run the
+// register-staged kernel.
+inline bool lds_fits(int M, int N, int K, int lda, int ldb, bool AT, bool BT, bool tail = false) {
+  if ((!AT || !BT) && K % 64 != 0 && !tail) return false;
   const unsigned long long lim = (1ull << 32) - 1;
   const unsigned long long a_bytes = static_cast<unsigned long long>(AT ? K : M) * lda * 2;
   const unsigned long long b_bytes = static_cast<unsigned long long>(BT ? K : N) * ldb * 2;

@@ -57,6 +57,7 @@ enum class Epi : int {
   // its gradient through the down-projection, N = F: with [g | u] = R[m, 2F]
   // and dh = acc, Y[m, 2F] = [dh u act'(g) | dh act(g)]      (bf16 out)
   kGluGrad = 8,
+  kPlainTail = 9,  // kPlain, over a contraction that need not be a multiple of 64
 };
 
 struct GemmArgs {

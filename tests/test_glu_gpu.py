@@ -26,7 +26,7 @@ STEPS = (1, 2, 3, 4, 5, 8, 20)
 def _cases(layout, steps):
     """Per tile the smallest size that runs on it, unsplit, at this contraction."""
     out = {}
-    for M, F in SIZES:
+    for M, F in SIZES:  # (the second size is the output's columns, of the forward's gates)
         if M * F * steps > 2.5e8:  # (the oracle's time)
             continue
         bm, bn, sp = B.linear_plan(layout, M, 2 * F if layout == B.LAYOUT_FWD_GELU else F, 64 * steps)
@@ -99,6 +99,63 @@ def test_contractions_that_are_no_multiple_of_64(M, H, F, act):
     _forward(M, H, F, act)
     _forward(M, H, F, act, bias=False, save=False)
     _backward(M, H, F, act)
+
+
+def _up_backward(M, H, F, split=True, seed=20):
+    announce(f"glu_up_bwd_data M={M} H={H} F={F} split={split}")
+    dgu, w = random_bf16((M, 2 * F), seed), random_bf16((2 * F, H), seed + 1, 1.0 / F ** 0.5)
+    dy, buf = guarded((M, H), BF)
+    B.enc_glu_up_bwd_data(cuda(dgu), cuda(w), dy2=dy, split=split)
+    torch.cuda.synchronize()
+    a, b = f64(dgu), f64(w)
+    ref, err = a @ b, (2 * F + 4) * P.FP32 * (np.abs(a) @ np.abs(b))
+    _within(dy, ref, P.BF16 * (np.abs(ref) + err) + err, f"{M}x{H}x{F}")
+    assert guard_intact(buf, dy.numel())
+
+
+@gpu
+@pytest.mark.parametrize("steps,more", [(0, 8), (0, 56), (1, 8), (1, 40), (2, 24), (3, 56), (4, 8), (5, 32), (8, 16)])
+def test_contractions_that_end_inside_a_step(steps, more):
+    """Every tile at contractions of whole steps and a part of one."""
+    K = 64 * steps + more
+    for i, (_, (M, F)) in enumerate(_cases(B.LAYOUT_FWD_GELU, steps + 1)):
+        _forward(M, K, F, "silu", bias=i % 2 == 0, seed=100 * i)
+    for i, (_, (M, F)) in enumerate(_cases(B.LAYOUT_DGRAD_GELU, steps + 1)):
+        _backward(M, K, F, "silu", seed=100 * i)
+    if K % 16 == 0:
+        for i, (_, (M, N)) in enumerate(_cases(B.LAYOUT_DGRAD, steps + 1)):
+            _up_backward(M, N, K // 2, seed=100 * i)
+
+
+@gpu
+@pytest.mark.parametrize("M,H,F", [(1, 8, 8), (70, 1280, 2056), (200, 1280, 2048), (520, 264, 100 * 8)])
+def test_up_backward(M, H, F):
+    for split in (True, False):
+        _up_backward(M, H, F, split)
+
+
+@gpu
+def test_a_row_does_not_reach_into_the_next():
+    """Contractions that end inside a step: the loads that would reach the next
+    row's first elements must not, which NaNs there would show."""
+    M, H, F = 140, 200, 104
+    announce("glu ragged contraction with NaN in one row")
+    y, w = random_bf16((M, H), 1), random_bf16((2 * F, H), 2, 0.1)
+    dout, w2, gu = random_bf16((M, H), 3), random_bf16((H, F), 4, 0.1), random_bf16((M, 2 * F), 5)
+    dgu, bad = random_bf16((M, 2 * F), 6), 77
+    for t in (y, dout, dgu):
+        t[bad] = float("nan")
+    _, h = B.enc_glu_up_fwd(cuda(y), cuda(w))
+    d = B.enc_glu_down_bwd_data(cuda(dout), cuda(w2), cuda(gu))
+    dy = B.enc_glu_up_bwd_data(cuda(dgu), cuda(w))
+    for t in (h, d, dy):
+        rows = torch.isnan(t.float()).any(1).cpu()
+        assert rows[bad] and int(rows.sum()) == 1
+    # and a NaN in the weight's row of one gate reaches that column only
+    w[5] = float("nan")
+    _, h = B.enc_glu_up_fwd(cuda(random_bf16((M, H), 1)), cuda(w))
+    cols = torch.isnan(h.float()).any(0).cpu()
+    assert cols[5] and int(cols.sum()) == 1
 
 
 @gpu
