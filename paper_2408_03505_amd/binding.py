@@ -162,22 +162,24 @@ def _call(name, *args):
 
 def _stream(stream):
     if stream is None:
-        stream = torch.cuda.current_stream()
-    return ctypes.c_void_p(stream.cuda_stream)
+        # the current stream's handle, without the Stream object around it
+        # (0.1 us; torch.cuda.current_stream() takes 2.6, as long as a launch)
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    return stream.cuda_stream
 
 
 def _ptr(t):
-    return ctypes.c_void_p(t.data_ptr()) if t is not None else ctypes.c_void_p(0)
+    return t.data_ptr() if t is not None else None
 
 
 def _check(t, name, shape, dtype=torch.bfloat16):
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
-    if t.device.type != "cuda":
+    if not t.is_cuda:
         raise ValueError(f"{name} must be a GPU tensor")
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape and tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
@@ -186,7 +188,7 @@ def _check(t, name, shape, dtype=torch.bfloat16):
 
 def _out(t, name, shape, like, dtype=torch.bfloat16):
     if t is None:
-        return torch.empty(shape, dtype=dtype, device=like.device)
+        return like.new_empty(shape, dtype=dtype)
     return _check(t, name, shape, dtype)
 
 
@@ -822,6 +824,12 @@ def enc_packed_plan(cu_seqlens, tokens, plan=None, stream=None):
     return plan
 
 
+def _check_plan(plan):
+    if not isinstance(plan, torch.Tensor):
+        raise TypeError("plan must be a torch.Tensor")
+    _check(plan, "plan", (plan.numel(),), torch.uint8)  # (its size is the library's to check)
+
+
 def attn_packed_bwd_workspace_bytes(tokens, heads):
     n = ctypes.c_size_t()
     _call("enc_attn_packed_bwd_workspace_bytes", tokens, heads, ctypes.byref(n))
@@ -834,7 +842,7 @@ def enc_attn_packed_fwd(seqs, heads, kv_heads, head_dim, qkv, plan, causal=False
     are (uninitialised where o or lse is not given)."""
     T = qkv.shape[0]
     _check(qkv, "qkv", (T, (heads + 2 * kv_heads) * head_dim))
-    _check(plan, "plan", (packed_plan_bytes(T, seqs),), torch.uint8)
+    _check_plan(plan)
     o = _out(o, "o", (T, heads * head_dim), qkv)
     lse = _out(lse, "lse", (heads, T), qkv, torch.float32)
     _call("enc_attn_packed_fwd", T, seqs, heads, kv_heads, head_dim, 1 if causal else 0, _ptr(plan), plan.numel(),
@@ -851,7 +859,7 @@ def enc_attn_packed_bwd(seqs, heads, kv_heads, head_dim, qkv, o, lse, do, plan, 
     _check(o, "o", (T, heads * head_dim))
     _check(lse, "lse", (heads, T), torch.float32)
     _check(do, "do", (T, heads * head_dim))
-    _check(plan, "plan", (packed_plan_bytes(T, seqs),), torch.uint8)
+    _check_plan(plan)
     dqkv = _out(dqkv, "dqkv", (T, width), qkv)
     if ws is None:
         ws = torch.empty(attn_packed_bwd_workspace_bytes(T, heads), dtype=torch.uint8, device=qkv.device)

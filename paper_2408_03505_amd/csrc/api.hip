@@ -301,6 +301,7 @@ bool gemm_wgrad(int M, int N, int K, const bf16_t *dY, const bf16_t *X, float *d
 // [g | u][M, 2F] = Y[M, H] Wgu[2F, H]^T + b; h[M, F] = act(g) u
 bool glu_fwd(int M, int F, int H, int act, const bf16_t *Y, const bf16_t *W, const bf16_t *b, bf16_t *gu, bf16_t *h,
              void *ws, size_t ws_bytes, hipStream_t s) {
+  if (glu_few_tokens(M, F, H)) return launch_glu_small(M, F, H, act, Y, W, b, gu, h, s);
   GemmArgs a{};
   a.M = M, a.N = 2 * F, a.K = H;
   a.A = Y, a.lda = H, a.B = W, a.ldb = H;

@@ -319,6 +319,16 @@ inline GemmPlan gemm_plan(int M, int N, int K, int lda, int ldb, bool AT, bool B
   return {any_tile(M, N), 1};
 }
 
+// Whether a gated feed-forward block's forward runs the kernel for few tokens.
+// That kernel reads the tokens' rows once per 8 columns of F, which costs M / 16
+// of the weights' bytes again, from the caches: nothing where its single launch
+// is the gain, a quarter of the time of a large weight.  At 16 tokens, us, against
+// the tiled product: 1280 x 3416 9.1 / 16.2, 6144 x 2048 18.4 / 21.8, but 6144 x
+// 16384 115 / 77-95; at 4 tokens there 79 / 78-95.
+inline bool glu_few_tokens(int M, int F, int K) {
+  return M <= 4 || (M <= 16 && 2ll * F * K <= (1ll << 25));
+}
+
 inline size_t ws_round256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 
 // Workspace of a split forward or input-gradient product: the fp32 partials

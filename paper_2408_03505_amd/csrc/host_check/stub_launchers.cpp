@@ -47,6 +47,9 @@ hipError_t attn_bwd_scratch(float **ptr) {
   *ptr = stand_in;
   return hipSuccess;
 }
+bool launch_glu_small(int, int, int, int, const bf16_t *, const bf16_t *, const bf16_t *, bf16_t *, bf16_t *, hipStream_t) {
+  return true;
+}
 bool launch_rope(const RopeArgs &, hipStream_t) { return true; }
 bool launch_packed_plan(int, int, const int *, PackedPlan *, hipStream_t) { return true; }
 bool launch_attn_packed_fwd(const PackedAttnArgs &, hipStream_t) { return true; }

@@ -98,6 +98,11 @@ bool launch_gemm_dgrad(const GemmArgs &a, Epi epi, void *ws, size_t ws_bytes, hi
 // ws = nullptr never splits.
 bool launch_gemm_wgrad(const GemmArgs &a, void *ws, size_t ws_bytes, hipStream_t s, FinishJobs *defer = nullptr);
 
+// ---- Gated feed-forward for up to 16 tokens: [g | u] = y Wgu^T + b (K columns),
+// h = act(g) u; gu and bias may be null.
+bool launch_glu_small(int M, int F, int K, int act, const bf16_t *y, const bf16_t *w, const bf16_t *bias, bf16_t *gu,
+                      bf16_t *h, hipStream_t s);
+
 // ---- QK normalisation (LayerNorm of every query and key vector over head_dim)
 bool launch_qk_norm_fwd(int M, int heads, int d, const bf16_t *qkv, const bf16_t *qg, const bf16_t *qb,
                         const bf16_t *kg, const bf16_t *kb, float eps, bf16_t *qkvn, float *stats, hipStream_t s);

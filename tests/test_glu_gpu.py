@@ -128,6 +128,15 @@ def test_contractions_that_end_inside_a_step(steps, more):
 
 
 @gpu
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("M", [1, 2, 4, 5, 15, 16, 17])
+def test_few_tokens(M, act):
+    """Sizes on both sides of the rule that picks the kernel for few tokens."""
+    for H, F in ((8, 8), (72, 40), (512, 24), (1288, 344), (2048, 520), (2056, 8200)):
+        _forward(M, H, F, act, bias=F != 344, save=F != 40, seed=M)
+
+
+@gpu
 @pytest.mark.parametrize("M,H,F", [(1, 8, 8), (70, 1280, 2056), (200, 1280, 2048), (520, 264, 100 * 8)])
 def test_up_backward(M, H, F):
     for split in (True, False):
