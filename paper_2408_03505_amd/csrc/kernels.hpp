@@ -138,6 +138,7 @@ bool launch_packed_plan(int tokens, int seqs, const int *cu, PackedPlan *plan, h
 
 struct PackedAttnArgs {
   int tokens, slots, heads, kv_heads, d, causal;
+  int shared4;  // set by the launchers: a multiple of four heads share their keys
   const PackedPlan *plan;
   const bf16_t *qkv;  // [tokens, (heads + 2 kv_heads) d]
   bf16_t *o;          // [tokens, heads d]
