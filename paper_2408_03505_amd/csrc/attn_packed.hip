@@ -530,27 +530,23 @@ packed_bwd_dq_kernel(PackedAttnArgs p) {
 // dP start from the dQ kernel's -lse sqrt(D) and -D_i, which lie in LDS in the
 // order of the result's registers, so neither is subtracted afterwards.
 
-// LDS of one stage: the Q and dO tiles, then -lse sqrt(D) and -D_i of up to 64 queries.
-template <int KT>
-constexpr int packed_dkdv_stage() {
-  return 2 * tile_bytes<KT>() + 2 * 64 * 4;
-}
+// LDS of one stage: the tiles of Q and dO, then -lse sqrt(D) and -D_i, for each of
+// which a wave loads 64 values (a tile has 32).
+constexpr int kDkvTiles = 2 * tile_bytes<32>(), kDkvStage = kDkvTiles + 2 * 64 * 4;
 
 // Wide heads keep the V rows in LDS: K, V and the two accumulators would leave
 // no registers to read operands ahead into.
 constexpr bool dkdv_v_in_lds(int d) { return d > 80; }
 
-template <int D, int NW, int KT, int MINB>
-__global__ __attribute__((amdgpu_flat_work_group_size(NW * 64, NW * 64), amdgpu_waves_per_eu(MINB, MINB))) void packed_bwd_dkdv_kernel(PackedAttnArgs p) {
+template <int D, int WPE>
+__global__ __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_waves_per_eu(WPE, WPE))) void
+packed_bwd_dkdv_kernel(PackedAttnArgs p) {
   using H = Head<D>;
-  static_assert(32 * NW == kPackedRows, "one item per workgroup");
-  constexpr int TB = tile_bytes<KT>(), TILES = 2 * TB;  // Q, dO
-  constexpr int STAGE = packed_dkdv_stage<KT>(), NS = KT / 32;
-  using Loads = PackedLoads<D, KT, NW>;
+  constexpr int KT = 32, TB = tile_bytes<KT>(), TILES = kDkvTiles, STAGE = kDkvStage;  // Q, dO, vectors
+  using Loads = PackedLoads<D, KT, 4>;
   constexpr bool VL = dkdv_v_in_lds(D);
   extern __shared__ __attribute__((aligned(1024))) char smem_raw[];
-  const lds_char *smem = (const lds_char *)(smem_raw);
-  const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(smem));
+  const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((const lds_char *)smem_raw));
 
   int item, kvh, first, len, row;
   packed_item(p.kv_heads, item, kvh);
@@ -630,44 +626,36 @@ __global__ __attribute__((amdgpu_flat_work_group_size(NW * 64, NW * 64), amdgpu_
     // query of the tile, only load and synchronise
     if (!active || (p.causal && q0 + KT <= k0w)) return;
     rd.local();
-    // register 4g+e of fragment f is query f*32 + 8g + 4hf + e
-    f32x16_t s[NS], dp[NS];
+    // register 4g + e is query 8g + 4 hf + e
+    f32x16_t sl, dp;
 #pragma unroll
-    for (int f = 0; f < NS; ++f) {
+    for (int g = 0; g < 4; ++g) {
+      const f32x4_t l4 = rd.vec(ST + TILES + g * 32), d4 = rd.vec(ST + TILES + 256 + g * 32);
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const f32x4_t l4 = rd.vec(ST + TILES + f * 128 + g * 32), d4 = rd.vec(ST + TILES + 256 + f * 128 + g * 32);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s[f][4 * g + e] = l4[e], dp[f][4 * g + e] = d4[e];
-      }
-#pragma unroll
-      for (int kk = 0; kk < H::KS; ++kk) s[f] = mfma32(rd.row(ST, f, kk), kf[kk], s[f]);
-#pragma unroll
-      for (int kk = 0; kk < H::KS; ++kk)
-        dp[f] = mfma32(rd.row(ST + TB, f, kk), VL ? rd.template at<bf16x8_t>(vown + kk * 1024) : vf[kk], dp[f]);
+      for (int e = 0; e < 4; ++e) sl[4 * g + e] = l4[e], dp[4 * g + e] = d4[e];
     }
 #pragma unroll
-    for (int f = 0; f < NS; ++f)
+    for (int kk = 0; kk < H::KS; ++kk) sl = mfma32(rd.row(ST, 0, kk), kf[kk], sl);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[f][i] = exp2_hw(s[f][i] * c);  // P
+    for (int kk = 0; kk < H::KS; ++kk)
+      dp = mfma32(rd.row(ST + TB, 0, kk), VL ? rd.template at<bf16x8_t>(vown + kk * 1024) : vf[kk], dp);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sl[i] = exp2_hw(sl[i] * c);  // P
     if (p.causal && q0 < k0w + 31) {  // some query of the tile precedes some key of the wave
 #pragma unroll
-      for (int f = 0; f < NS; ++f)
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (q0 + f * 32 + (i >> 2) * 8 + hf * 4 + (i & 3) < key) s[f][i] = 0.f;
+      for (int i = 0; i < 16; ++i)
+        if (q0 + (i >> 2) * 8 + hf * 4 + (i & 3) < key) sl[i] = 0.f;
     }
 #pragma unroll
-    for (int st = 0; st < KT / 16; ++st) {
-      const bf16x8_t pb = pack8(s[st >> 1], st & 1);
+    for (int st = 0; st < 2; ++st) {
+      const bf16x8_t pb = pack8(sl, st);
 #pragma unroll
       for (int nf = 0; nf < H::NF; ++nf) dv[nf] = mfma32(rd.col(ST + TB, nf, st), pb, dv[nf]);
     }
+    dp *= sl;  // dS
 #pragma unroll
-    for (int f = 0; f < NS; ++f) dp[f] *= s[f];  // dS
-#pragma unroll
-    for (int st = 0; st < KT / 16; ++st) {
-      const bf16x8_t sb = pack8(dp[st >> 1], st & 1);
+    for (int st = 0; st < 2; ++st) {
+      const bf16x8_t sb = pack8(dp, st);
 #pragma unroll
       for (int nf = 0; nf < H::NF; ++nf) dk[nf] = mfma32(rd.col(ST, nf, st), sb, dk[nf]);
     }
@@ -678,30 +666,27 @@ __global__ __attribute__((amdgpu_flat_work_group_size(NW * 64, NW * 64), amdgpu_
   }
   block_barrier();  // the output slots reuse the tile buffers
   bf16_t *out = p.dqkv + static_cast<size_t>(first + k0w) * ld + A + kvh * D;
-  lds_char *slot = const_cast<lds_char *>(smem) + wid * 8192;
+  lds_char *slot = (lds_char *)smem_raw + wid * 8192;
   store_dmajor_lds<D>(out, ld, dk, 1.0f / sqrtf(static_cast<float>(D)), lane, slot, len - k0w);
   store_dmajor_lds<D>(out + p.kv_heads * D, ld, dv, 1.0f, lane, slot, len - k0w);
 }
 
-// Launch shapes: 4 waves of 32 queries (forward, dQ) or keys (dK/dV); KT is the
-// token tile streamed through LDS, MINB the workgroups each CU must hold at once.
-constexpr int kDkvWaves = 4, kDkvKT = 32, kDkvMinBlocks = 2;
+// Waves per SIMD: as many as the registers of one allow.  LDS: the tiles' stages,
+// which the waves' output slots of 8 KB reuse.
+constexpr int kOutLds = 4 * 8192;
 
 template <int D>
 void launch_fwd_d(const PackedAttnArgs &a, hipStream_t s) {
-  // the stages of K and V tiles; the per-wave 8 KB output slots reuse them
-  constexpr int lds = std::max(4 * tile_bytes<32>(), 4 * 8192), waves = D == 64 ? 4 : D == 80 ? 3 : 2;
+  constexpr int lds = std::max(4 * tile_bytes<32>(), kOutLds), waves = D == 64 ? 4 : D == 80 ? 3 : 2;
   hipLaunchKernelGGL((packed_fwd_kernel<D, waves>), dim3(a.slots * a.heads), dim3(256), lds, s, a);
 }
 
 template <int D>
 void launch_bwd_d(const PackedAttnArgs &a, hipStream_t s) {
-  constexpr int kDqLds = std::max(5 * tile_bytes<32>(), 4 * 8192), waves = D == 128 ? 2 : 3;
-  constexpr int kDkvLds =
-      std::max(2 * packed_dkdv_stage<kDkvKT>() + (dkdv_v_in_lds(D) ? kDkvWaves * 32 * D * 2 : 0), kDkvWaves * 8192);
-  hipLaunchKernelGGL((packed_bwd_dq_kernel<D, waves>), dim3(a.slots * a.heads), dim3(256), kDqLds, s, a);
-  hipLaunchKernelGGL((packed_bwd_dkdv_kernel<D, kDkvWaves, kDkvKT, kDkvMinBlocks>), dim3(a.slots * a.kv_heads),
-                     dim3(kDkvWaves * 64), kDkvLds, s, a);
+  constexpr int dq_lds = std::max(5 * tile_bytes<32>(), kOutLds), dq_waves = D == 128 ? 2 : 3;
+  constexpr int dkdv_lds = std::max(2 * kDkvStage + (dkdv_v_in_lds(D) ? 4 * 32 * D * 2 : 0), kOutLds);
+  hipLaunchKernelGGL((packed_bwd_dq_kernel<D, dq_waves>), dim3(a.slots * a.heads), dim3(256), dq_lds, s, a);
+  hipLaunchKernelGGL((packed_bwd_dkdv_kernel<D, D == 64 ? 3 : 2>), dim3(a.slots * a.kv_heads), dim3(256), dkdv_lds, s, a);
 }
 
 PackedAttnArgs with_shared4(const PackedAttnArgs &args) {
