@@ -66,7 +66,7 @@ struct PackedItem {
 };
 
 struct PackedPlan {
-  int count, pad[3];
+  int count, pad[3];  // count: the list's items, without the empty ones
   PackedItem item[1];
 };
 

@@ -3,8 +3,8 @@
 //
 // Pair i of every query and key vector is turned by pos[row, axis(i)] *
 // inv_freq[i]; the backward turns it back (a rotation's transpose is its
-// inverse), so one kernel serves both.  The values are copied, unless the
-// output is the input.
+// inverse), so one kernel serves both.  Pairs without an axis and the values are
+// copied (the values not where the output is the input).
 //
 // Bound by memory: 4 bytes per element (read and written once) and one angle
 // per row and pair, shared by all heads.  A workgroup takes one row: it
@@ -55,12 +55,10 @@ __global__ __launch_bounds__(256) void rope_kernel(int M, int qk_heads, int v_he
     lo = ldg16(x + base + at(tid));
     hi = ldg16(x + base + at(tid) + HALF);
   }
-  if (tid < HALF) {
-    float c = 1.f, s = 0.f;
-    if (tid < used) {
-      const int axis = tid < sec_t ? 0 : tid < sec_th ? 1 : 2;
-      angle_of(pos[static_cast<size_t>(row) * 3 + axis], inv_freq[tid], c, s);
-    }
+  if (tid < used) {
+    const int axis = tid < sec_t ? 0 : tid < sec_th ? 1 : 2;
+    float c, s;
+    angle_of(pos[static_cast<size_t>(row) * 3 + axis], inv_freq[tid], c, s);
     cs[tid] = c;
     sn[tid] = s * sign;
   }
@@ -83,13 +81,14 @@ __global__ __launch_bounds__(256) void rope_kernel(int M, int qk_heads, int v_he
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int j = c8 / 2 + e;
-        turn(p[2 * e], p[2 * e + 1], cs[j], sn[j]);
-        turn(q[2 * e], q[2 * e + 1], cs[j + HALF / 2], sn[j + HALF / 2]);
+        if (j < used) turn(p[2 * e], p[2 * e + 1], cs[j], sn[j]);
+        if (j + HALF / 2 < used) turn(q[2 * e], q[2 * e + 1], cs[j + HALF / 2], sn[j + HALF / 2]);
       }
     } else {
       // pairs (j, j + D / 2): one member in each chunk
 #pragma unroll
-      for (int e = 0; e < 8; ++e) turn(p[e], q[e], cs[c8 + e], sn[c8 + e]);
+      for (int e = 0; e < 8; ++e)
+        if (c8 + e < used) turn(p[e], q[e], cs[c8 + e], sn[c8 + e]);
     }
     u32x4_t o0, o1;
 #pragma unroll

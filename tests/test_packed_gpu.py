@@ -74,6 +74,25 @@ def test_rope_of_negative_positions():
     within(y, ref, P.rope_bound(f64(x), ref, 2, 2, 64, pos.numpy(), f.numpy(), (8, 12, 12), False))
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("d, sec", [(64, (0, 0, 0)), (80, (3, 0, 8)), (128, (16, 24, 23))])
+def test_rope_copies_pairs_without_an_axis_bit_for_bit(d, sec, interleaved):
+    """Signed zeros, infinities and NaN among them, which a turn by no angle would not keep."""
+    x, pos, f = _rope_inputs(5, 3, 1, d, sec, 50, 3)
+    used, i = sum(sec), torch.arange(sum(sec), d // 2)
+    a, b = (2 * i, 2 * i + 1) if interleaved else (i, i + d // 2)
+    heads = x.view(5, 5, d)
+    heads[:, :, a] = -0.0
+    heads[0, :, b], heads[1, :, b], heads[2, :, b], heads[3, :, b] = float("inf"), float("nan"), float("-inf"), 0.0
+    announce(f"rope d={d} sections={sec} interleaved={interleaved} non-finite pairs without an axis")
+    for call in (B.enc_rope_fwd, B.enc_rope_bwd):
+        y = call(3, 1, d, cuda(x), cuda(pos), cuda(f), sec, interleaved).cpu().view(5, 5, d)
+        for c in (a, b):
+            assert torch.equal(y[:, :, c].view(torch.int16), heads[:, :, c].view(torch.int16))
+        turned = [c for c in range(d) if c not in a.tolist() + b.tolist()]
+        assert len(turned) == 2 * used and torch.isfinite(y[:, :, turned]).all()
+
+
 # ------------------------------------------------------------------ work list
 
 def _items(plan):
