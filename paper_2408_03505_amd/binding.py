@@ -172,11 +172,14 @@ def _ptr(t):
     return t.data_ptr() if t is not None else None
 
 
-def _check(t, name, shape, dtype=torch.bfloat16):
+def _check(t, name, shape, dtype=torch.bfloat16, dev=None):
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
-    if not t.is_cuda:
+    on = t.get_device()
+    if on < 0:
         raise ValueError(f"{name} must be a GPU tensor")
+    if dev is not None and on != dev:
+        raise ValueError(f"{name} is on device {on}, the current device is {dev}")
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     if t.shape != shape and tuple(t.shape) != tuple(shape):
@@ -186,10 +189,33 @@ def _check(t, name, shape, dtype=torch.bfloat16):
     return t
 
 
-def _out(t, name, shape, like, dtype=torch.bfloat16):
+def _out(t, name, shape, like, dtype=torch.bfloat16, stream=None, dev=None):
     if t is None:
-        return like.new_empty(shape, dtype=dtype)
-    return _check(t, name, shape, dtype)
+        return like.new_empty(shape, dtype=dtype) if stream is None else _empty(like.new_empty, shape, dtype, stream)
+    return _check(t, name, shape, dtype, dev)
+
+
+def _empty(new, shape, dtype, stream, **where):
+    """A fresh tensor for a call on `stream`, from that stream's memory: memory of the
+    current one may still be in use there, or be given to its next call before
+    `stream` is done with it."""
+    if stream is None:
+        return new(shape, dtype=dtype, **where)
+    with torch.cuda.stream(stream):
+        return new(shape, dtype=dtype, **where)
+
+
+def _device(x, stream, ws=None):
+    """The current device, on which the library launches: the calls that ask refuse a
+    stream, a workspace or (_check) any tensor of another one."""
+    if x.get_device() < 0:
+        return -1  # a host tensor, which _check refuses
+    dev = torch._C._cuda_getDevice()
+    if stream is not None and stream.device_index != dev:
+        raise ValueError(f"stream is of device {stream.device_index}, the current device is {dev}")
+    if ws is not None and ws.get_device() != dev:
+        raise ValueError(f"ws is on device {ws.get_device()}, the current device is {dev}")
+    return dev
 
 
 def make_cfg(cfg):
@@ -444,7 +470,7 @@ def linear_plan(layout, M, N, K):
     return r.value, c.value, sp.value
 
 
-def _gemm_ws(M, N, K, ws, split, device):
+def _gemm_ws(M, N, K, ws, split, device, stream=None):
     """Workspace argument of a forward or input-gradient product with output
     [M, N] and contraction K: a caller tensor, a fresh one of the queried
     size (split=True, ws=None), or none (split=False)."""
@@ -454,11 +480,11 @@ def _gemm_ws(M, N, K, ws, split, device):
         need = linear_workspace_bytes(M, N, K)
         if need == 0:
             return ctypes.c_void_p(0), 0
-        ws = torch.empty(need, dtype=torch.uint8, device=device)
+        ws = _empty(torch.empty, need, torch.uint8, stream, device=device)
     return _ptr(ws), ws.numel() * ws.element_size()
 
 
-def _wgrad_ws(M, N, K, ws, split, device):
+def _wgrad_ws(M, N, K, ws, split, device, stream=None):
     """Workspace argument of a weight-gradient call: a caller tensor, a fresh
     one of the queried size (split=True, ws=None), or none (split=False)."""
     if not split:
@@ -467,7 +493,7 @@ def _wgrad_ws(M, N, K, ws, split, device):
         need = linear_bwd_weight_workspace_bytes(M, N, K)
         if need == 0:
             return ctypes.c_void_p(0), 0
-        ws = torch.empty(need, dtype=torch.uint8, device=device)
+        ws = _empty(torch.empty, need, torch.uint8, stream, device=device)
     return _ptr(ws), ws.numel() * ws.element_size()
 
 
@@ -488,7 +514,7 @@ def enc_linear_bwd_weight(dY, X, dW=None, db=None, accumulate=False, with_db=Tru
 
 
 def _named_wgrad(name, M, a, b, N, K, dY, X, dW, db, accumulate, ws, split, stream):
-    wp, wn = _wgrad_ws(M, N, K, ws, split, dY.device)
+    wp, wn = _wgrad_ws(M, N, K, ws, split, dY.device, stream)
     _call(name, M, a, b, _ptr(dY), _ptr(X), _ptr(dW), _ptr(db), 1 if accumulate else 0, wp, wn, _stream(stream))
     return dW, db
 
@@ -780,10 +806,11 @@ def enc_qkv_bwd_data_add(dqkv, w_qkv, addend, dy=None, ws=None, split=True, stre
 def _rope(name, in_name, out_name, heads, kv_heads, head_dim, x, pos, inv_freq, sections, interleaved, y, stream):
     M = x.shape[0]
     width = (heads + 2 * kv_heads) * head_dim
-    _check(x, in_name, (M, width))
-    _check(pos, "pos", (M, 3), torch.int32)
-    _check(inv_freq, "inv_freq", (head_dim // 2,), torch.float32)
-    y = _out(y, out_name, (M, width), x)
+    dev = _device(x, stream)
+    _check(x, in_name, (M, width), dev=dev)
+    _check(pos, "pos", (M, 3), torch.int32, dev=dev)
+    _check(inv_freq, "inv_freq", (head_dim // 2,), torch.float32, dev=dev)
+    y = _out(y, out_name, (M, width), x, stream=stream, dev=dev)
     sec_t, sec_h, sec_w = sections
     _call(name, M, heads, kv_heads, head_dim, sec_t, sec_h, sec_w, 1 if interleaved else 0, _ptr(x), _ptr(pos),
           _ptr(inv_freq), _ptr(y), _stream(stream))
@@ -818,16 +845,17 @@ def enc_packed_plan(cu_seqlens, tokens, plan=None, stream=None):
     if not isinstance(cu_seqlens, torch.Tensor) or cu_seqlens.dim() != 1 or cu_seqlens.shape[0] < 2:
         raise ValueError("cu_seqlens must be a tensor of seqs + 1 offsets")
     seqs = cu_seqlens.shape[0] - 1
-    _check(cu_seqlens, "cu_seqlens", (seqs + 1,), torch.int32)
-    plan = _out(plan, "plan", (packed_plan_bytes(tokens, seqs),), cu_seqlens, torch.uint8)
+    dev = _device(cu_seqlens, stream)
+    _check(cu_seqlens, "cu_seqlens", (seqs + 1,), torch.int32, dev=dev)
+    plan = _out(plan, "plan", (packed_plan_bytes(tokens, seqs),), cu_seqlens, torch.uint8, stream, dev=dev)
     _call("enc_packed_plan", tokens, seqs, _ptr(cu_seqlens), _ptr(plan), plan.numel(), _stream(stream))
     return plan
 
 
-def _check_plan(plan):
+def _check_plan(plan, dev):
     if not isinstance(plan, torch.Tensor):
         raise TypeError("plan must be a torch.Tensor")
-    _check(plan, "plan", (plan.numel(),), torch.uint8)  # (its size is the library's to check)
+    _check(plan, "plan", (plan.numel(),), torch.uint8, dev=dev)  # (its size is the library's to check)
 
 
 def attn_packed_bwd_workspace_bytes(tokens, heads):
@@ -841,10 +869,11 @@ def enc_attn_packed_fwd(seqs, heads, kv_heads, head_dim, qkv, plan, causal=False
     heads * head_dim], lse [heads, tokens]); rows of no sequence are left as they
     are (uninitialised where o or lse is not given)."""
     T = qkv.shape[0]
-    _check(qkv, "qkv", (T, (heads + 2 * kv_heads) * head_dim))
-    _check_plan(plan)
-    o = _out(o, "o", (T, heads * head_dim), qkv)
-    lse = _out(lse, "lse", (heads, T), qkv, torch.float32)
+    dev = _device(qkv, stream)
+    _check(qkv, "qkv", (T, (heads + 2 * kv_heads) * head_dim), dev=dev)
+    _check_plan(plan, dev)
+    o = _out(o, "o", (T, heads * head_dim), qkv, stream=stream, dev=dev)
+    lse = _out(lse, "lse", (heads, T), qkv, torch.float32, stream, dev=dev)
     _call("enc_attn_packed_fwd", T, seqs, heads, kv_heads, head_dim, 1 if causal else 0, _ptr(plan), plan.numel(),
           _ptr(qkv), _ptr(o), _ptr(lse), _stream(stream))
     return o, lse
@@ -855,14 +884,15 @@ def enc_attn_packed_bwd(seqs, heads, kv_heads, head_dim, qkv, o, lse, do, plan, 
     """Gradient of enc_attn_packed_fwd; rows of no sequence are left as they are."""
     T = qkv.shape[0]
     width = (heads + 2 * kv_heads) * head_dim
-    _check(qkv, "qkv", (T, width))
-    _check(o, "o", (T, heads * head_dim))
-    _check(lse, "lse", (heads, T), torch.float32)
-    _check(do, "do", (T, heads * head_dim))
-    _check_plan(plan)
-    dqkv = _out(dqkv, "dqkv", (T, width), qkv)
+    dev = _device(qkv, stream, ws)
+    _check(qkv, "qkv", (T, width), dev=dev)
+    _check(o, "o", (T, heads * head_dim), dev=dev)
+    _check(lse, "lse", (heads, T), torch.float32, dev=dev)
+    _check(do, "do", (T, heads * head_dim), dev=dev)
+    _check_plan(plan, dev)
+    dqkv = _out(dqkv, "dqkv", (T, width), qkv, stream=stream, dev=dev)
     if ws is None:
-        ws = torch.empty(attn_packed_bwd_workspace_bytes(T, heads), dtype=torch.uint8, device=qkv.device)
+        ws = _empty(qkv.new_empty, attn_packed_bwd_workspace_bytes(T, heads), torch.uint8, stream)
     _call("enc_attn_packed_bwd", T, seqs, heads, kv_heads, head_dim, 1 if causal else 0, _ptr(plan), plan.numel(),
           _ptr(qkv), _ptr(o), _ptr(lse), _ptr(do), _ptr(dqkv), _ptr(ws), ws.numel() * ws.element_size(),
           _stream(stream))
@@ -881,16 +911,17 @@ def enc_glu_up_fwd(y2, w_gu, b_gu=None, act=GLU_SILU, gu=None, h=None, save=True
     F2 = w_gu.shape[0]
     if F2 % 2:
         raise ValueError("w_gu rows must be 2*F")
-    _check(y2, "y2", (M, H))
-    _check(w_gu, "w_gu", (F2, H))
+    dev = _device(y2, stream, ws)
+    _check(y2, "y2", (M, H), dev=dev)
+    _check(w_gu, "w_gu", (F2, H), dev=dev)
     if b_gu is not None:
-        _check(b_gu, "b_gu", (F2,))
+        _check(b_gu, "b_gu", (F2,), dev=dev)
     if save:
-        gu = _out(gu, "gu", (M, F2), y2)
+        gu = _out(gu, "gu", (M, F2), y2, stream=stream, dev=dev)
     elif gu is not None:
         raise ValueError("gu given with save=False")
-    h = _out(h, "h", (M, F2 // 2), y2)
-    wp, wn = _gemm_ws(M, F2, H, ws, split, y2.device)
+    h = _out(h, "h", (M, F2 // 2), y2, stream=stream, dev=dev)
+    wp, wn = _gemm_ws(M, F2, H, ws, split, y2.device, stream)
     _call("enc_glu_up_fwd", M, H, F2 // 2, act, _ptr(y2), _ptr(w_gu), _ptr(b_gu), _ptr(gu), _ptr(h), wp, wn,
           _stream(stream))
     return gu, h
@@ -899,11 +930,12 @@ def enc_glu_up_fwd(y2, w_gu, b_gu=None, act=GLU_SILU, gu=None, h=None, save=True
 def enc_glu_down_bwd_data(dout, w_2, gu, act=GLU_SILU, dgu=None, ws=None, split=True, stream=None):
     M, H = dout.shape
     F = w_2.shape[1]
-    _check(dout, "dout", (M, H))
-    _check(w_2, "w_2", (H, F))
-    _check(gu, "gu", (M, 2 * F))
-    dgu = _out(dgu, "dgu", (M, 2 * F), dout)
-    wp, wn = _gemm_ws(M, F, H, ws, split, dout.device)
+    dev = _device(dout, stream, ws)
+    _check(dout, "dout", (M, H), dev=dev)
+    _check(w_2, "w_2", (H, F), dev=dev)
+    _check(gu, "gu", (M, 2 * F), dev=dev)
+    dgu = _out(dgu, "dgu", (M, 2 * F), dout, stream=stream, dev=dev)
+    wp, wn = _gemm_ws(M, F, H, ws, split, dout.device, stream)
     _call("enc_glu_down_bwd_data", M, F, H, act, _ptr(dout), _ptr(w_2), _ptr(gu), _ptr(dgu), wp, wn, _stream(stream))
     return dgu
 
@@ -913,10 +945,11 @@ def enc_glu_up_bwd_data(dgu, w_gu, dy2=None, ws=None, split=True, stream=None):
     H = w_gu.shape[1]
     if F2 % 2:
         raise ValueError("dgu columns must be 2*F")
-    _check(dgu, "dgu", (M, F2))
-    _check(w_gu, "w_gu", (F2, H))
-    dy2 = _out(dy2, "dy2", (M, H), dgu)
-    wp, wn = _gemm_ws(M, H, F2, ws, split, dgu.device)
+    dev = _device(dgu, stream, ws)
+    _check(dgu, "dgu", (M, F2), dev=dev)
+    _check(w_gu, "w_gu", (F2, H), dev=dev)
+    dy2 = _out(dy2, "dy2", (M, H), dgu, stream=stream, dev=dev)
+    wp, wn = _gemm_ws(M, H, F2, ws, split, dgu.device, stream)
     _call("enc_glu_up_bwd_data", M, H, F2 // 2, _ptr(dgu), _ptr(w_gu), _ptr(dy2), wp, wn, _stream(stream))
     return dy2
 
@@ -926,10 +959,11 @@ def enc_glu_up_bwd_weight(dgu, y2, dw_gu, db_gu=None, accumulate=False, ws=None,
     H = y2.shape[1]
     if F2 % 2:
         raise ValueError("dgu columns must be 2*F")
-    _check(dgu, "dgu", (M, F2)); _check(y2, "y2", (M, H))
-    _check(dw_gu, "dw_gu", (F2, H), torch.float32)
+    dev = _device(dgu, stream, ws)
+    _check(dgu, "dgu", (M, F2), dev=dev); _check(y2, "y2", (M, H), dev=dev)
+    _check(dw_gu, "dw_gu", (F2, H), torch.float32, dev=dev)
     if db_gu is not None:
-        _check(db_gu, "db_gu", (F2,), torch.float32)
+        _check(db_gu, "db_gu", (F2,), torch.float32, dev=dev)
     return _named_wgrad("enc_glu_up_bwd_weight", M, H, F2 // 2, F2, H, dgu, y2, dw_gu, db_gu, accumulate, ws, split,
                         stream)
 

@@ -261,6 +261,60 @@ def test_attention_is_deterministic_and_replays_from_a_graph():
         torch.cuda.synchronize()
 
 
+def test_a_stream_of_the_callers_gets_memory_of_its_own():
+    """Outputs and workspaces of a call on another stream lie in none of the current
+    stream's memory: there the writes of a freed tensor may still be on their way."""
+    heads, d, T = 16, 128, 4096
+    announce("packed attention on a side stream, outputs not given")
+    qkv, do = cuda(random_bf16((T, 3 * heads * d), 43)), cuda(random_bf16((T, heads * d), 44))
+    plan = _plan([0, T], T)
+    o, lse = B.enc_attn_packed_fwd(1, heads, heads, d, qkv, plan)
+    dqkv = B.enc_attn_packed_bwd(1, heads, heads, d, qkv, o, lse, do, plan)
+    y, w = do[:256].contiguous(), cuda(random_bf16((4096, heads * d), 45))
+    gu, h = B.enc_glu_up_fwd(y, w)
+    torch.cuda.synchronize()
+    want = [t.cpu() for t in (o, lse, dqkv, gu, h)]
+    shapes = [(t.shape, t.dtype) for t in (o, lse, dqkv, gu, h)]
+    side = torch.cuda.Stream()
+    old = [torch.empty(s, dtype=t, device="cuda") for s, t in shapes]
+    for _ in range(200):
+        for t in old:
+            t.fill_(1.5)
+    del old, t
+    po, plse = B.enc_attn_packed_fwd(1, heads, heads, d, qkv, plan, stream=side)
+    pdqkv = B.enc_attn_packed_bwd(1, heads, heads, d, qkv, po, plse, do, plan, stream=side)
+    pgu, ph = B.enc_glu_up_fwd(y, w, stream=side)
+    torch.cuda.synchronize()
+    assert all(torch.equal(t.cpu(), v) for t, v in zip((po, plse, pdqkv, pgu, ph), want))
+
+
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    """(This process has one device: the current one is made to look like another.)"""
+    qkv = cuda(random_bf16((4, 3 * 64), 46))
+    plan = _plan([0, 4], 4)
+    o, lse = B.enc_attn_packed_fwd(1, 1, 1, 64, qkv, plan)
+    torch.cuda.synchronize()
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1)
+    x, w = o, torch.zeros(16, 64, dtype=BF, device=o.device)
+    pos, freq = torch.zeros(4, 3, dtype=torch.int32, device=o.device), torch.ones(32, device=o.device)
+    cu = torch.tensor([0, 4], dtype=torch.int32, device=o.device)
+    side = torch.cuda.Stream(device=0)
+    for call in (lambda s: B.enc_rope_fwd(1, 1, 64, qkv, pos, freq, (8, 8, 8), stream=s),
+                 lambda s: B.enc_rope_bwd(1, 1, 64, qkv, pos, freq, (8, 8, 8), stream=s),
+                 lambda s: B.enc_packed_plan(cu, 4, stream=s),
+                 lambda s: B.enc_attn_packed_fwd(1, 1, 1, 64, qkv, plan, stream=s),
+                 lambda s: B.enc_attn_packed_bwd(1, 1, 1, 64, qkv, o, lse, o, plan, stream=s),
+                 lambda s: B.enc_glu_up_fwd(x, w, stream=s),
+                 lambda s: B.enc_glu_down_bwd_data(x, w[:8].t().contiguous(), torch.cat([x, x])[:4, :16].contiguous(),
+                                                   stream=s),
+                 lambda s: B.enc_glu_up_bwd_data(x[:, :16].contiguous(), w, stream=s),
+                 lambda s: B.enc_glu_up_bwd_weight(x[:, :16].contiguous(), x, torch.zeros(16, 64, device=o.device),
+                                                   stream=s)):
+        for s in (None, side):
+            with pytest.raises(ValueError, match="the current device is 1"):
+                call(s)
+
+
 def test_attention_at_the_end_of_the_largest_tensor():
     """The last rows of a qkv of nearly 2^31 elements (4 GiB), whose last tile
     would reach past 32-bit byte offsets."""
