@@ -79,8 +79,8 @@ int check_mult8(const char *fn, std::initializer_list<int> dims) {
 // but tile indices and row counts are 32-bit).
 constexpr long kMaxElems = 1L << 31;
 
-// Packed sequences: the work list compares every pair of them, and a head
-// count and a sequence count this size keep every grid below 2^32 threads.
+// Packed sequences: the work list compares every pair of them, and heads times
+// head_dim is an int.
 constexpr int kMaxSeqs = 65536, kMaxHeads = 65536;
 
 // A launcher refused a shape that the argument checks accepted.  The checks
@@ -461,7 +461,7 @@ int attn_packed_dims(const char *fn, int tokens, int seqs, int heads, int kv_hea
   int r = packed_dims(fn, tokens, heads, kv_heads, d);
   if (r || (r = packed_seqs(fn, tokens, seqs))) return r;
   if (causal != 0 && causal != 1) return fail(ENC_ERR_INVALID, "%s: causal must be 0 or 1", fn);
-  // workgroups of 256 threads, two per item in the dK/dV kernel: fewer than 2^32 threads
+  // workgroups of 256 threads, one per item and head: fewer than 2^31 threads
   if (static_cast<long>(packed_slots(tokens, seqs)) * heads >= 1L << 23)
     return fail(ENC_ERR_UNSUPPORTED, "%s: (tokens / 128 + seqs) * heads must be below 2^23", fn);
   return ENC_OK;

@@ -11,17 +11,29 @@
 // The mathematics and the products' orientation are those of the dense
 // attention kernels (S^T = K Q^T, O^T += V^T P^T, online softmax with a lazily
 // moved maximum; the backward recomputes P from lse).  What differs:
-//  - Every tile is loaded through a buffer resource of its own, which begins at
-//    the tile's first row (64-bit, so a tensor may be as long as memory holds)
-//    and ends with the sequence's last row: rows past it read as zero, and a
-//    non-finite value behind a sequence never reaches it.  Lanes whose LDS
-//    columns lie past the head's width ask for nothing.
+//  - A sequence's tiles of one head are loaded through one buffer resource, which
+//    begins at its first row (a 64-bit address) and ends with its last: rows past
+//    it read as zero, and a non-finite value behind a sequence never reaches it.
+//    Lanes whose LDS columns lie past the head's width ask for nothing.
 //  - With `causal`, a query's keys end with itself: key tiles past a
 //    workgroup's last query (query tiles before its first key, in dK/dV) are
 //    skipped, and those on the diagonal are masked element by element.
 //  - dK/dV runs over the queries of every head that shares the key head, in
 //    head order, so the gradients of shared heads are summed in the
 //    accumulators, with no atomics and always in the same order.
+//
+// What bounds it: the matrix cores under the card's power limit on long sequences
+// (16 heads of 128 over 7936 + 515 + 1 tokens: busy 0.53 of the time at 1.9 GHz in
+// the forward, 0.66 at 1.7 in dQ, 0.61 at 1.85 in dK/dV), with as many LDS bytes
+// as the LDS can deliver beside them (each 32x32x16 product reads 1 KB, which takes
+// the CU as long as its four SIMDs take to use it).  On short and ragged ones (40
+// images of 68 to 1020 tokens, 16 heads of 80: 0.35 to 0.39 busy at 2.05 GHz) the
+// latency of one wave's chain of products, exponentials and LDS reads, with the
+// workgroups' starts, ends and half-empty last tiles; below some 200 tokens each
+// kernel is bound by its bytes (112 x 128 tokens, 16 heads of 80: forward 31 us for
+// 147 MB, backward 97 for 441).  Figures beside the kernels are medians of a kernel
+// trace; rates count 4, 6 and 8 flops per query, key and element of a head in the
+// forward, dQ (S, dP and dQ) and dK/dV (S, dP, dV and dK).
 #include <math.h>
 
 #include <algorithm>
@@ -65,7 +77,7 @@ __device__ __forceinline__ bool load_item(const PackedPlan *plan, int tokens, in
 // and first query, and the keys that some query of it sees.  Four waves take an
 // item's 128 queries of one head; or, where a multiple of four heads share their
 // keys, 32 queries of four heads.  Then the waves see the same keys with `causal`
-// too, and fewer waves lie past a sequence's end (24 prompts of 30 to 2048
+// too, and fewer waves lie past a sequence's end (24 prompts of 30 to 1625
 // tokens, 32 heads on 8, causal: forward 126 -> 116 us, dQ 195 -> 184).
 struct QueryWork {
   int first, len;     // the sequence
@@ -208,6 +220,12 @@ struct PackedReads {
 // turn and three waves per SIMD, the matrix cores were busy 0.45 of the time and
 // the vector units 0.45.)  Tile t + 2's keys and tile t + 1's values are loaded
 // meanwhile.
+//
+// 16 heads of 128 over 7936 + 515 + 1 tokens 488 us (1060 TFLOP/s); 16 of 80 over
+// the 40 images 71 (660); 32 of 128 on 8, causal, 24 prompts of 30 to 1625 tokens
+// 144 (680; 117 in a loop of this kernel alone).  A tile's loads, LDS reads and
+// exponentials, each left out of a copy, took 18, 61 and 13 us of 523 at 8192
+// tokens: none alone is what it waits for.
 
 // The next N instructions of a kind in the order wanted of the scheduler.
 constexpr int kSchedVector = 0x2, kSchedMfma = 0x8, kSchedLds = 0x100, kSchedTrans = 0x400;
@@ -385,6 +403,9 @@ packed_fwd_kernel(PackedAttnArgs p) {
 // V dO^T is in one piece of code with the exponentials of tile t, S(t + 1) with
 // dS(t) = P (dP - D), and dQ^T += K^T dS^T follows.  Three stages of K (tile t
 // for dQ, t + 1 for S, t + 2 in flight) and two of V.
+//
+// The three sets as for the forward: 653 us (1190 TFLOP/s), 99 (700), 199 (740).
+// It also leaves -lse sqrt(D) and -D_i for the dK/dV kernel.
 
 template <int D, int WPE>
 __global__ __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_waves_per_eu(WPE, WPE))) void
@@ -529,6 +550,11 @@ packed_bwd_dq_kernel(PackedAttnArgs p) {
 // full-rate vector instructions and 16 exponentials.  The accumulators of S and
 // dP start from the dQ kernel's -lse sqrt(D) and -D_i, which lie in LDS in the
 // order of the result's registers, so neither is subtracted afterwards.
+//
+// The three sets as for the forward: 879 us (1180 TFLOP/s), 127 (730), 288 (680;
+// its longest workgroup takes 204 tiles in turn, four heads' 51).  64 keys
+// per wave, which would halve the LDS reads, leave one wave per SIMD and were
+// slower; so was V in registers at D = 128 (spills).
 
 // LDS of one stage: the tiles of Q and dO, then -lse sqrt(D) and -D_i, for each of
 // which a wave loads 64 values (a tile has 32).
@@ -686,7 +712,8 @@ void launch_bwd_d(const PackedAttnArgs &a, hipStream_t s) {
   constexpr int dq_lds = std::max(5 * tile_bytes<32>(), kOutLds), dq_waves = D == 128 ? 2 : 3;
   constexpr int dkdv_lds = std::max(2 * kDkvStage + (dkdv_v_in_lds(D) ? 4 * 32 * D * 2 : 0), kOutLds);
   hipLaunchKernelGGL((packed_bwd_dq_kernel<D, dq_waves>), dim3(a.slots * a.heads), dim3(256), dq_lds, s, a);
-  hipLaunchKernelGGL((packed_bwd_dkdv_kernel<D, D == 64 ? 3 : 2>), dim3(a.slots * a.kv_heads), dim3(256), dkdv_lds, s, a);
+  constexpr int dkdv_waves = D == 64 ? 3 : 2;
+  hipLaunchKernelGGL((packed_bwd_dkdv_kernel<D, dkdv_waves>), dim3(a.slots * a.kv_heads), dim3(256), dkdv_lds, s, a);
 }
 
 PackedAttnArgs with_shared4(const PackedAttnArgs &args) {
