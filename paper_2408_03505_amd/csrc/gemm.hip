@@ -39,20 +39,24 @@ namespace {
 
 // Eight outputs of a gated block, gate g and up-projection u in fp32:
 // h = act(g) u, and [g | u] themselves where they are kept.
+// Stored for the caches to keep, for the product that reads them next: with
+// streaming stores the two input gradients at 5003 x 1280 x 3416 took 181 us, not
+// 158, at 2048 x 6144 x 2048 153, not 145, the forward at 5003 x 1280 x 3416 107,
+// not 100.
 __device__ __forceinline__ void glu_store8(const float (&g)[8], const float (&u)[8], int act, bf16_t *gu_g,
                                            bf16_t *gu_u, bf16_t *h) {
   u32x4_t o;
   if (gu_g) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[e] = pack2(g[2 * e], g[2 * e + 1]);
-    stg16_nt(gu_g, o);
+    stg16(gu_g, o);
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[e] = pack2(u[2 * e], u[2 * e + 1]);
-    stg16_nt(gu_u, o);
+    stg16(gu_u, o);
   }
 #pragma unroll
   for (int e = 0; e < 4; ++e) o[e] = pack2(gate_f(g[2 * e], act) * u[2 * e], gate_f(g[2 * e + 1], act) * u[2 * e + 1]);
-  stg16_nt(h, o);
+  stg16(h, o);
 }
 
 // Their gradients [dh u act'(g) | dh act(g)] from the saved g and u.
@@ -66,8 +70,8 @@ __device__ __forceinline__ void glu_grad_store8(const float (&dh)[8], u32x4_t gw
     o[e] = pack2(dh[2 * e] * lo_bf(uw[e]) * d0, dh[2 * e + 1] * hi_bf(uw[e]) * d1);
     w[e] = pack2(dh[2 * e] * v0, dh[2 * e + 1] * v1);
   }
-  stg16_nt(dg, o);
-  stg16_nt(du, w);
+  stg16(dg, o);
+  stg16(du, w);
 }
 
 // Whether an epilogue evaluates an activation (those products have rows of the
