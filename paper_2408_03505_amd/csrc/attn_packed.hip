@@ -159,12 +159,37 @@ struct PackedLoads {
   }
 };
 
+// LDS address of this lane's first transposed read of a tile's columns D - 16 ..
+// D - 1 as the operand of a 16x16x32 product: lanes 16 g .. 16 g + 15 read the eight
+// tokens that 16-lane groups of a packed result hold (Result::add), 4 (g / 2) + 16
+// (g % 2) and those 8 further on (second_read's).
+template <int D, bool PERM>
+__device__ __forceinline__ int tail_first(int lane, uint32_t lds0) {
+  const int g = lane >> 4, k = 16 * (g & 1) + (PERM ? 4 : 8) * (g >> 1) + ((lane & 15) >> 2);
+  const int n = D - 16 + 4 * (lane & 3);
+  return lds0 + tile_off(k, n >> 3) + (n & 7) * 2;
+}
+// 8 rows further with PERM, else 4 (the swizzle differs in one bit)
+template <bool PERM>
+__device__ __forceinline__ int second_read(int c) {
+  return PERM ? (c ^ 32) + 8 * kDL * 2 : (c ^ 16) + 4 * kDL * 2;
+}
+
 // TileReads with every address a whole LDS address, so that stage, tile,
 // fragment and step all go in the reads' offset field.
 template <int D, bool PERM>
 struct PackedReadsR {
   TileReads<D, PERM> t;
-  __device__ __forceinline__ void init(int lane, uint32_t lds0) { t.init(lane, lds0, lds0); }
+  int tail_off[2];
+  __device__ __forceinline__ void init(int lane, uint32_t lds0) {
+    t.init(lane, lds0, lds0);
+    tail_off[0] = tail_first<D, PERM>(lane, lds0);
+    tail_off[1] = second_read<PERM>(tail_off[0]);
+  }
+  __device__ __forceinline__ bf16x8_t tail(int base) const {
+    return lds_read_tr(reinterpret_cast<const lds_char *>(static_cast<uint32_t>(tail_off[0] + base)),
+                       reinterpret_cast<const lds_char *>(static_cast<uint32_t>(tail_off[1] + base)));
+  }
   __device__ __forceinline__ bf16x8_t row(int base, int f, int kk) const {
     return *reinterpret_cast<const __attribute__((address_space(3))) bf16x8_t *>(
         static_cast<uint32_t>(t.row_off[kk] + base + f * 32 * kDL * 2));
@@ -182,13 +207,14 @@ struct PackedReadsR {
 // instruction per read, where registers are what limits the kernel.
 template <int D, bool PERM>
 struct PackedReads {
-  int row0, col0, vec0;
+  int row0, col0, vec0, tail0;
   __device__ __forceinline__ void init(int lane, uint32_t lds0) {
     row0 = lds0 + tile_off(lane & 31, lane >> 5);
     const int k = (PERM ? 4 : 8) * (lane >> 5) + ((lane & 15) >> 2);
     const int n = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
     col0 = lds0 + tile_off(k, n >> 3) + (n & 7) * 2;
     vec0 = lds0 + (lane >> 5) * 16;
+    tail0 = tail_first<D, PERM>(lane, lds0);
     asm volatile("" : "+v"(row0), "+v"(col0), "+v"(vec0));
   }
   // Called in the loop: keeps its addresses from being computed, and held in
@@ -201,13 +227,104 @@ struct PackedReads {
   __device__ __forceinline__ bf16x8_t row(int base, int f, int kk) const {
     return at<bf16x8_t>((row0 ^ (kk << 5)) + base + f * 32 * kDL * 2);
   }
-  // the second read: 8 rows further with PERM (tsw differs in one bit), else 4
   __device__ __forceinline__ bf16x8_t col(int base, int nf, int st) const {
     const int o = base + st * 16 * kDL * 2, c = col0 ^ (nf << 6);
-    const int c1 = PERM ? (c ^ 32) + 8 * kDL * 2 : (c ^ 16) + 4 * kDL * 2;
-    return lds_read_tr(reinterpret_cast<const lds_char *>(c + o), reinterpret_cast<const lds_char *>(c1 + o));
+    return lds_read_tr(reinterpret_cast<const lds_char *>(c + o),
+                       reinterpret_cast<const lds_char *>(second_read<PERM>(c) + o));
+  }
+  __device__ __forceinline__ bf16x8_t tail(int base) const {
+    return lds_read_tr(reinterpret_cast<const lds_char *>(tail0 + base),
+                       reinterpret_cast<const lds_char *>(second_read<PERM>(tail0) + base));
   }
   __device__ __forceinline__ f32x4_t vec(int base) const { return at<f32x4_t>(vec0 + base); }
+};
+
+// A value of each lane's token (lane % 32) for results that hold tokens 0..15 (lo)
+// and 16..31 (hi) in every 16 lanes.
+__device__ __forceinline__ void by_halves(uint32_t a, uint32_t b, uint32_t &lo, uint32_t &hi) {
+  const auto r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+  lo = r[0];
+  hi = r[1];
+}
+__device__ __forceinline__ void by_halves(float v, float &lo, float &hi) {
+  uint32_t a, b;
+  by_halves(__float_as_uint(v), __float_as_uint(v), a, b);
+  lo = __uint_as_float(a);
+  hi = __uint_as_float(b);
+}
+
+// The sum of tiles' products with a 32x32 result, [D][32 tokens]: fragments of 32
+// rows, and for a head that ends with 16 more (80) two of 16 by 16 tokens, where a
+// third 32-row fragment would spend twice the matrix and LDS time on them.
+template <int D>
+struct Result {
+  static constexpr int NF = D / 32;
+  static constexpr bool TAIL = D % 32 != 0;
+  static_assert(!TAIL || D % 32 == 16, "a half fragment at the end");
+  static constexpr int MFMAS = 2 * NF + 2 * TAIL, READS = 4 * NF + 2 * TAIL;  // of add
+  f32x16_t w[NF];
+  f32x4_t t[2];
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int i = 0; i < NF; ++i) w[i] = f32x16_t{};
+    t[0] = t[1] = f32x4_t{};
+  }
+  // each token's column by the value of its lanes
+  __device__ __forceinline__ void scale(float s) {
+#pragma unroll
+    for (int i = 0; i < NF; ++i) w[i] *= s;
+    if constexpr (TAIL) {
+      float lo, hi;
+      by_halves(s, lo, hi);
+      t[0] *= lo;
+      t[1] *= hi;
+    }
+  }
+  // += X^T s, s a 32x32 result [token of the tile][token], X the tile at base.
+  // s is rounded to bf16 here, the matrix cores' operand.
+  template <class Reads>
+  __device__ __forceinline__ void add(const Reads &rd, int base, const f32x16_t &s) {
+    bf16x8_t b[2];
+#pragma unroll
+    for (int st = 0; st < 2; ++st) {
+      b[st] = pack8(s, st);
+#pragma unroll
+      for (int i = 0; i < NF; ++i) w[i] = mfma32(rd.col(base, i, st), b[st], w[i]);
+    }
+    if constexpr (TAIL) {
+      // Lanes 16 r .. 16 r + 15 of b[st] hold tokens 16 (r % 2) .. + 15 and, of the
+      // tile, 4 (r / 2) + 16 st ..; the product takes all of one half's tokens.
+      const u32x4_t x = __builtin_bit_cast(u32x4_t, b[0]), y = __builtin_bit_cast(u32x4_t, b[1]);
+      u32x4_t lo, hi;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        uint32_t l, h;
+        by_halves(x[e], y[e], l, h);
+        lo[e] = l;
+        hi[e] = h;
+      }
+      const bf16x8_t v = rd.tail(base);
+      t[0] = mfma16(v, as_bf16x8(lo), t[0]);
+      t[1] = mfma16(v, as_bf16x8(hi), t[1]);
+    }
+  }
+  // times s, through the wave's LDS slot, to rows dst, dst + ld ..
+  __device__ __forceinline__ void store(bf16_t *dst, size_t ld, float s, int lane, lds_char *slot, int ntok) const {
+    dmajor_to_lds<D>(w, s, lane, slot);
+    if constexpr (TAIL) {
+      float lo, hi;
+      by_halves(s, lo, hi);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int tok = 16 * i + (lane & 15), c = D / 8 - 2 + (lane >> 5);
+        const float f = i ? hi : lo;
+        *reinterpret_cast<__attribute__((address_space(3))) u32x2_t *>(slot + tok * 256 + ((c ^ (tok & 15)) << 4) +
+                                                                        ((lane >> 4) & 1) * 8) =
+            u32x2_t{pack2(t[i][0] * f, t[i][1] * f), pack2(t[i][2] * f, t[i][3] * f)};
+      }
+    }
+    store_rows_lds<D>(dst, ld, lane, slot, ntok);
+  }
 };
 
 // ------------------------------------------------------------------ forward
@@ -273,9 +390,8 @@ packed_fwd_kernel(PackedAttnArgs p) {
   bf16x8_t qf[H::KS];
   load_row_operand<D>(qf, seq + static_cast<size_t>(q) * ld + h * D, q < len, hf);
 
-  f32x16_t acc[H::NF];
-#pragma unroll
-  for (int i = 0; i < H::NF; ++i) acc[i] = f32x16_t{};
+  Result<D> acc;
+  acc.zero();
   float m = -INFINITY, top = -INFINITY, l = 0.f;
   const float c = kLog2e / sqrtf(static_cast<float>(D));
 
@@ -312,8 +428,7 @@ packed_fwd_kernel(PackedAttnArgs p) {
       m = mn;
       top = (mn + kLazyRescale) / c;
       l *= alpha;
-#pragma unroll
-      for (int nf = 0; nf < H::NF; ++nf) acc[nf] *= alpha;
+      acc.scale(alpha);
     }
   };
 
@@ -352,12 +467,7 @@ packed_fwd_kernel(PackedAttnArgs p) {
       l1 += s[i + 1];
     }
     l += l0 + l1;
-#pragma unroll
-    for (int st = 0; st < 2; ++st) {
-      const bf16x8_t pb = pack8(s, st);
-#pragma unroll
-      for (int nf = 0; nf < H::NF; ++nf) acc[nf] = mfma32(rd.col(VB + ST * TB, nf, st), pb, acc[nf]);
-    }
+    acc.add(rd, VB + ST * TB, s);
     float ms = max16(next);
     // The order wanted: the keys' operands, under whose latency the first
     // exponentials run, then S(t + 1) with the other exponentials and the values'
@@ -370,10 +480,10 @@ packed_fwd_kernel(PackedAttnArgs p) {
       sched_group<kSchedMfma, 1>();
       sched_group<kSchedVector, 20 / H::KS>();
       sched_group<kSchedTrans, (8 + H::KS - 1) / H::KS>();
-      sched_group<kSchedLds, (4 * H::NF + H::KS - 1) / H::KS>();
+      sched_group<kSchedLds, (Result<D>::READS + H::KS - 1) / H::KS>();
     }
 #pragma unroll
-    for (int i = 0; i < 2 * H::NF; ++i) {
+    for (int i = 0; i < Result<D>::MFMAS; ++i) {
       sched_group<kSchedMfma, 1>();
       sched_group<kSchedVector, 2>();
     }
@@ -393,8 +503,8 @@ packed_fwd_kernel(PackedAttnArgs p) {
 
   const float lt = l + __shfl_xor(l, 32, kWave);
   if (q < len && hf == 0) p.lse[static_cast<size_t>(h) * p.tokens + first + q] = (m + log2f(lt)) / kLog2e;
-  store_dmajor_lds<D>(p.o + static_cast<size_t>(first + q0) * A + h * D, A, acc, 1.0f / lt, lane,
-                      (lds_char *)smem_raw + wid * 8192, len - q0);
+  acc.store(p.o + static_cast<size_t>(first + q0) * A + h * D, A, 1.0f / lt, lane, (lds_char *)smem_raw + wid * 8192,
+            len - q0);
 }
 
 // ------------------------------------------------------------------ backward: dQ and D
@@ -455,9 +565,8 @@ packed_bwd_dq_kernel(PackedAttnArgs p) {
     p.ndvec[vec] = -dd;
   }
 
-  f32x16_t acc[H::NF];
-#pragma unroll
-  for (int i = 0; i < H::NF; ++i) acc[i] = f32x16_t{};
+  Result<D> acc;
+  acc.zero();
   const int nk = (w.keys + KT - 1) / KT, nkw = (w.wave_keys + KT - 1) / KT;
   const int tmask = w.all_see / KT;
   const int lim = p.causal ? min(len, q + 1) : len;
@@ -522,12 +631,7 @@ packed_bwd_dq_kernel(PackedAttnArgs p) {
       for (int i = 0; i < 16; ++i)
         if ((i >> 2) * 8 + (i & 3) >= left) s[i] = 0.f;
     }
-#pragma unroll
-    for (int st = 0; st < 2; ++st) {
-      const bf16x8_t sb = pack8(s, st);
-#pragma unroll
-      for (int nf = 0; nf < H::NF; ++nf) acc[nf] = mfma32(rd.col(KS0, nf, st), sb, acc[nf]);
-    }
+    acc.add(rd, KS0, s);
   };
   for (int t = 0; t < nk; t += 6) {
     tile(Stage<0>(), Stage<0>(), s0, s1, t);
@@ -538,8 +642,8 @@ packed_bwd_dq_kernel(PackedAttnArgs p) {
     if (t + 5 < nk) tile(Stage<2>(), Stage<1>(), s1, s0, t + 5);
   }
   block_barrier();  // the output slots reuse the tile buffers
-  store_dmajor_lds<D>(p.dqkv + static_cast<size_t>(first + q0) * ld + h * D, ld, acc,
-                      1.0f / sqrtf(static_cast<float>(D)), lane, (lds_char *)smem_raw + wid * 8192, len - q0);
+  acc.store(p.dqkv + static_cast<size_t>(first + q0) * ld + h * D, ld, 1.0f / sqrtf(static_cast<float>(D)), lane,
+            (lds_char *)smem_raw + wid * 8192, len - q0);
 }
 
 // ------------------------------------------------------------------ backward: dK, dV
@@ -631,9 +735,9 @@ packed_bwd_dkdv_kernel(PackedAttnArgs p) {
         *reinterpret_cast<__attribute__((address_space(3))) bf16x8_t *>(vown + kk * 1024) = vf[kk];
     }
   }
-  f32x16_t dk[H::NF], dv[H::NF];
-#pragma unroll
-  for (int i = 0; i < H::NF; ++i) dk[i] = f32x16_t{}, dv[i] = f32x16_t{};
+  Result<D> dk, dv;
+  dk.zero();
+  dv.zero();
   const float c = kLog2e / sqrtf(static_cast<float>(D));
   PackedReads<D, true> rd;
   rd.init(lane, lds0);
@@ -672,19 +776,9 @@ packed_bwd_dkdv_kernel(PackedAttnArgs p) {
       for (int i = 0; i < 16; ++i)
         if (q0 + (i >> 2) * 8 + hf * 4 + (i & 3) < key) sl[i] = 0.f;
     }
-#pragma unroll
-    for (int st = 0; st < 2; ++st) {
-      const bf16x8_t pb = pack8(sl, st);
-#pragma unroll
-      for (int nf = 0; nf < H::NF; ++nf) dv[nf] = mfma32(rd.col(ST + TB, nf, st), pb, dv[nf]);
-    }
+    dv.add(rd, ST + TB, sl);
     dp *= sl;  // dS
-#pragma unroll
-    for (int st = 0; st < 2; ++st) {
-      const bf16x8_t sb = pack8(dp, st);
-#pragma unroll
-      for (int nf = 0; nf < H::NF; ++nf) dk[nf] = mfma32(rd.col(ST, nf, st), sb, dk[nf]);
-    }
+    dk.add(rd, ST, dp);
   };
   for (int n = 0; n < total; n += 2) {
     tile(Stage<0>(), n);
@@ -693,8 +787,8 @@ packed_bwd_dkdv_kernel(PackedAttnArgs p) {
   block_barrier();  // the output slots reuse the tile buffers
   bf16_t *out = p.dqkv + static_cast<size_t>(first + k0w) * ld + A + kvh * D;
   lds_char *slot = (lds_char *)smem_raw + wid * 8192;
-  store_dmajor_lds<D>(out, ld, dk, 1.0f / sqrtf(static_cast<float>(D)), lane, slot, len - k0w);
-  store_dmajor_lds<D>(out + p.kv_heads * D, ld, dv, 1.0f, lane, slot, len - k0w);
+  dk.store(out, ld, 1.0f / sqrtf(static_cast<float>(D)), lane, slot, len - k0w);
+  dv.store(out + p.kv_heads * D, ld, 1.0f, lane, slot, len - k0w);
 }
 
 // Waves per SIMD: as many as the registers of one allow.  LDS: the tiles' stages,

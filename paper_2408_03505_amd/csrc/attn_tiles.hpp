@@ -49,14 +49,12 @@ __device__ __forceinline__ void load_row_operand(bf16x8_t (&f)[Head<D>::KS], con
 // per instruction; here the runs go to LDS row t (256-byte rows, 16-byte
 // chunk c stored at c ^ (t % 16)), and each lane then writes whole 16-byte
 // row segments: a quarter-wave covers one row, four rows per instruction.
-// dst is the row of the wave's first token, ld the row stride (elements),
-// ntok the wave's tokens inside the sequence (the rest are not stored).
-template <int D>
-__device__ __forceinline__ void store_dmajor_lds(bf16_t *dst, size_t ld, const f32x16_t (&acc)[Head<D>::NF], float s,
-                                                 int lane, lds_char *slot, int ntok) {
+// First half: the runs of fragments 0 .. NF - 1, up to row D, into the slot.
+template <int D, int NF>
+__device__ __forceinline__ void dmajor_to_lds(const f32x16_t (&acc)[NF], float s, int lane, lds_char *slot) {
   const int t = lane & 31, hf = lane >> 5;
 #pragma unroll
-  for (int nf = 0; nf < Head<D>::NF; ++nf) {
+  for (int nf = 0; nf < NF; ++nf) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const int d0 = nf * 32 + q * 8 + hf * 4;
@@ -68,6 +66,13 @@ __device__ __forceinline__ void store_dmajor_lds(bf16_t *dst, size_t ld, const f
       }
     }
   }
+}
+
+// Second half: rows of D from the slot.  dst is the row of the wave's first
+// token, ld the row stride (elements), ntok the wave's tokens inside the
+// sequence (the rest are not stored).
+template <int D>
+__device__ __forceinline__ void store_rows_lds(bf16_t *dst, size_t ld, int lane, const lds_char *slot, int ntok) {
   // LDS accesses of one wave run in order: the reads below see the writes
   const int j = lane & 15;
 #pragma unroll
@@ -79,6 +84,13 @@ __device__ __forceinline__ void store_dmajor_lds(bf16_t *dst, size_t ld, const f
       stg16(dst + r * ld + j * 8, v);
     }
   }
+}
+
+template <int D>
+__device__ __forceinline__ void store_dmajor_lds(bf16_t *dst, size_t ld, const f32x16_t (&acc)[Head<D>::NF], float s,
+                                                 int lane, lds_char *slot, int ntok) {
+  dmajor_to_lds<D>(acc, s, lane, slot);
+  store_rows_lds<D>(dst, ld, lane, slot, ntok);
 }
 
 constexpr int kDL = 128;  // LDS row length (elements)
