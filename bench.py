@@ -234,7 +234,7 @@ TRAFFIC_MD = os.path.join(ROOT, "profiles", "vit22b_layer_hbm_traffic.md")
 # argument structs they receive and the launch geometry): traffic counters
 # describe these files only.
 _COMMON_SRC = ("common.hpp", "lds_dma.hpp", "kernels.hpp", "geometry.hpp")
-_FAMILY_SRC = {"gemm": ("gemm.hip", "reduce.hpp"), "attention": ("attention.hip",),
+_FAMILY_SRC = {"gemm": ("gemm.hip", "gate.hpp", "reduce.hpp"), "attention": ("attention.hip", "attn_tiles.hpp"),
                "layernorm": ("layernorm.hip", "reduce.hpp")}
 
 
