@@ -456,6 +456,11 @@ packed_fwd_kernel(PackedAttnArgs p) {
     if (t + 2 < nk) lk.template issue<ST * TB>();
     if (t + 1 < nk) lv.template issue<(1 - ST) * TB>();
     if (t >= nkw) return;  // waves that see none of the tile's keys only load and synchronise
+    // A wave's products go before the other waves' loads and prologues: from S(t + 1)
+    // on, 16 heads of 128 over 8192 tokens 553 -> 535 us, of 64 295 -> 287, but of 80,
+    // with three workgroups to a CU, 368 -> 385; there from P V on, 361.
+    constexpr bool kFromLogits = D != 80;
+    if constexpr (kFromLogits) __builtin_amdgcn_s_setprio(1);
     // (past the wave's last tile the logits are of stale data and not used)
     logits((1 - ST) * TB, next);
     float l0 = 0.f, l1 = 0.f;
@@ -467,7 +472,9 @@ packed_fwd_kernel(PackedAttnArgs p) {
       l1 += s[i + 1];
     }
     l += l0 + l1;
+    if constexpr (!kFromLogits) __builtin_amdgcn_s_setprio(1);
     acc.add(rd, VB + ST * TB, s);
+    __builtin_amdgcn_s_setprio(0);
     float ms = max16(next);
     // The order wanted: the keys' operands, under whose latency the first
     // exponentials run, then S(t + 1) with the other exponentials and the values'
