@@ -23,11 +23,11 @@
 //    accumulators, with no atomics and always in the same order.
 //
 // What bounds it: the matrix cores under the card's power limit on long sequences
-// (16 heads of 128 over 7936 + 515 + 1 tokens: busy 0.53 of the time at 1.9 GHz in
-// the forward, 0.66 at 1.7 in dQ, 0.61 at 1.85 in dK/dV), with as many LDS bytes
+// (16 heads of 128 over 7936 + 515 + 1 tokens: busy 0.59 of the time at 1.8 GHz in
+// the forward, 0.67 at 1.7 in dQ, 0.61 at 1.85 in dK/dV), with as many LDS bytes
 // as the LDS can deliver beside them (each 32x32x16 product reads 1 KB, which takes
 // the CU as long as its four SIMDs take to use it).  On short and ragged ones (40
-// images of 68 to 1020 tokens, 16 heads of 80: 0.35 to 0.39 busy at 2.05 GHz) the
+// images of 68 to 1020 tokens, 16 heads of 80: 0.32 to 0.37 busy at 2.05 GHz) the
 // latency of one wave's chain of products, exponentials and LDS reads, with the
 // workgroups' starts, ends and half-empty last tiles; below some 200 tokens each
 // kernel is bound by its bytes (112 x 128 tokens, 16 heads of 80: forward 31 us for
@@ -255,7 +255,8 @@ __device__ __forceinline__ void by_halves(float v, float &lo, float &hi) {
 
 // The sum of tiles' products with a 32x32 result, [D][32 tokens]: fragments of 32
 // rows, and for a head that ends with 16 more (80) two of 16 by 16 tokens, where a
-// third 32-row fragment would spend twice the matrix and LDS time on them.
+// third 32-row fragment would spend twice the matrix and LDS time on them (8192
+// tokens, 16 heads of 80: forward 374 -> 366 us, backward 1136 -> 1099).
 template <int D>
 struct Result {
   static constexpr int NF = D / 32;
@@ -338,9 +339,9 @@ struct Result {
 // the vector units 0.45.)  Tile t + 2's keys and tile t + 1's values are loaded
 // meanwhile.
 //
-// 16 heads of 128 over 7936 + 515 + 1 tokens 488 us (1060 TFLOP/s); 16 of 80 over
-// the 40 images 71 (660); 32 of 128 on 8, causal, 24 prompts of 30 to 1625 tokens
-// 144 (680; 117 in a loop of this kernel alone).  A tile's loads, LDS reads and
+// 16 heads of 128 over 7936 + 515 + 1 tokens 473 us (1100 TFLOP/s); 16 of 80 over
+// the 40 images 69 (670); 32 of 128 on 8, causal, 24 prompts of 30 to 1625 tokens
+// 141 (700; 118 in a loop of this kernel alone).  A tile's loads, LDS reads and
 // exponentials, each left out of a copy, took 18, 61 and 13 us of 523 at 8192
 // tokens: none alone is what it waits for.
 
@@ -521,7 +522,7 @@ packed_fwd_kernel(PackedAttnArgs p) {
 // dS(t) = P (dP - D), and dQ^T += K^T dS^T follows.  Three stages of K (tile t
 // for dQ, t + 1 for S, t + 2 in flight) and two of V.
 //
-// The three sets as for the forward: 653 us (1190 TFLOP/s), 99 (700), 199 (740).
+// The three sets as for the forward: 651 us (1190 TFLOP/s), 97 (720), 200 (730).
 // It also leaves -lse sqrt(D) and -D_i for the dK/dV kernel.
 
 template <int D, int WPE>
@@ -662,10 +663,11 @@ packed_bwd_dq_kernel(PackedAttnArgs p) {
 // dP start from the dQ kernel's -lse sqrt(D) and -D_i, which lie in LDS in the
 // order of the result's registers, so neither is subtracted afterwards.
 //
-// The three sets as for the forward: 879 us (1180 TFLOP/s), 127 (730), 288 (680;
+// The three sets as for the forward: 878 us (1180 TFLOP/s), 125 (740), 287 (680;
 // its longest workgroup takes 204 tiles in turn, four heads' 51).  64 keys
 // per wave, which would halve the LDS reads, leave one wave per SIMD and were
-// slower; so was V in registers at D = 128 (spills).
+// slower; so was V in registers at D = 128 (spills).  Query tiles from the last
+// down, which all of a sequence's workgroups would read together, gave nothing.
 
 // LDS of one stage: the tiles of Q and dO, then -lse sqrt(D) and -D_i, for each of
 // which a wave loads 64 values (a tile has 32).
