@@ -151,7 +151,7 @@ LENS = {
 
 @pytest.mark.parametrize("causal", [False, True])
 @pytest.mark.parametrize("heads,kv,d", [(3, 3, 64), (4, 2, 80), (8, 1, 128), (16, 16, 64), (16, 8, 80), (6, 3, 128),
-                                        (16, 2, 128)])
+                                        (16, 2, 128), (32, 8, 64), (4, 1, 80), (12, 3, 128)])
 @pytest.mark.parametrize("lens", sorted(LENS))
 def test_attention(lens, heads, kv, d, causal):
     lens = LENS[lens]
@@ -199,6 +199,20 @@ def test_attention_of_large_logits(d):
     within(lse, rlse, lbound)
     ref, bound = P.packed_attention_bwd(f64(qkv), cu, heads, heads, d, False, f64(do))
     within(dqkv, ref, bound)
+
+
+@pytest.mark.parametrize("heads,kv,d", [(2, 2, 64), (4, 1, 80), (2, 1, 128)])
+def test_a_later_token_reaches_no_earlier_tile(heads, kv, d):
+    """With causal attention, non-finite keys and values from token 200 on leave the
+    queries of the 32-token tiles before it as they are."""
+    announce(f"packed attention heads={heads}/{kv} d={d} non-finite later tokens")
+    qkv, _, _ = _attn_inputs([0, 300], 300, heads, kv, d, 27)
+    plan = _plan([0, 300], 300)
+    want, wlse = B.enc_attn_packed_fwd(1, heads, kv, d, cuda(qkv), plan, True)
+    for bad in (float("inf"), float("-inf"), float("nan")):
+        qkv[200:, heads * d:] = bad
+        o, lse = B.enc_attn_packed_fwd(1, heads, kv, d, cuda(qkv), plan, True)
+        assert torch.equal(o[:192], want[:192]) and torch.equal(lse[:, :192], wlse[:, :192])
 
 
 def test_attention_equals_the_dense_kernels_results():
