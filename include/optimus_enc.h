@@ -538,10 +538,15 @@ enum enc_glu_act {
   ENC_GLU_GELU = 1  /* act(g) = g Phi(g) (exact erf form) */
 };
 
+/* The workspace that the block's products (output [M, N], contraction K) make use
+ * of: enc_linear_workspace_bytes where K is a multiple of 64, and where it is not
+ * what splitting it takes.  A smaller one splits it into fewer parts. */
+int enc_glu_workspace_bytes(int M, int N, int K, size_t *bytes);
 /* [Gated block step: both up-projections, the activation and the product]
  * y2 [M, H]; b_gu [2F] or NULL; h [M, F] bf16, from g and u in fp32; gu
  * [M, 2F] or NULL (it is kept for the backward only).  ws: as for the other
- * products, enc_linear_workspace_bytes(M, 2F, H). */
+ * products, NULL or at least enc_linear_workspace_bytes(M, 2F, H);
+ * enc_glu_workspace_bytes(M, 2F, H) is what it makes use of, the same or more. */
 int enc_glu_up_fwd(int M, int H, int F, int act, const enc_bf16 *y2, const enc_bf16 *w_gu, const enc_bf16 *b_gu,
                    enc_bf16 *gu, enc_bf16 *h, void *ws, size_t ws_bytes, enc_stream_t stream);
 /* [Backward of the gated block's down-projection, product and activation]

@@ -115,6 +115,7 @@ _SIGS = {
     "enc_attn_packed_fwd": [_i, _i, _i, _i, _i, _i, _p, _sz, _p, _p, _p, _p],
     "enc_attn_packed_bwd_workspace_bytes": [_i, _i, ctypes.POINTER(_sz)],
     "enc_attn_packed_bwd": [_i, _i, _i, _i, _i, _i, _p, _sz, _p, _p, _p, _p, _p, _p, _sz, _p],
+    "enc_glu_workspace_bytes": [_i, _i, _i, ctypes.POINTER(_sz)],
     "enc_glu_up_fwd": [_i, _i, _i, _i, _p, _p, _p, _p, _p, _p, _sz, _p],
     "enc_glu_down_bwd_data": [_i, _i, _i, _i, _p, _p, _p, _p, _p, _sz, _p],
     "enc_glu_up_bwd_data": [_i, _i, _i, _p, _p, _p, _p, _sz, _p],
@@ -453,10 +454,14 @@ def linear_bwd_weight_workspace_bytes(M, N, K):
     return n.value
 
 
-def linear_workspace_bytes(M, N, K):
+def _ws_bytes(query, *dims):
     n = _sz()
-    _call("enc_linear_workspace_bytes", M, N, K, ctypes.byref(n))
+    _call(query, *dims, ctypes.byref(n))
     return n.value
+
+
+def linear_workspace_bytes(M, N, K):
+    return _ws_bytes("enc_linear_workspace_bytes", M, N, K)
 
 
 LAYOUT_FWD, LAYOUT_DGRAD, LAYOUT_WGRAD, LAYOUT_FWD_GELU, LAYOUT_DGRAD_GELU = 0, 1, 2, 3, 4
@@ -470,14 +475,14 @@ def linear_plan(layout, M, N, K):
     return r.value, c.value, sp.value
 
 
-def _gemm_ws(M, N, K, ws, split, device, stream=None):
+def _gemm_ws(M, N, K, ws, split, device, stream=None, query="enc_linear_workspace_bytes"):
     """Workspace argument of a forward or input-gradient product with output
     [M, N] and contraction K: a caller tensor, a fresh one of the queried
     size (split=True, ws=None), or none (split=False)."""
     if not split:
         return ctypes.c_void_p(0), 0
     if ws is None:
-        need = linear_workspace_bytes(M, N, K)
+        need = _ws_bytes(query, M, N, K)
         if need == 0:
             return ctypes.c_void_p(0), 0
         ws = _empty(torch.empty, need, torch.uint8, stream, device=device)
@@ -904,6 +909,10 @@ def enc_attn_packed_bwd(seqs, heads, kv_heads, head_dim, qkv, o, lse, do, plan, 
 GLU_SILU, GLU_GELU = 0, 1
 
 
+def glu_workspace_bytes(M, N, K):
+    return _ws_bytes("enc_glu_workspace_bytes", M, N, K)
+
+
 def enc_glu_up_fwd(y2, w_gu, b_gu=None, act=GLU_SILU, gu=None, h=None, save=True, ws=None, split=True, stream=None):
     """h = act(g) * u with [g | u] = y2 w_gu^T + b_gu.  Returns (gu, h); with
     save=False gu is not written (None)."""
@@ -921,7 +930,7 @@ def enc_glu_up_fwd(y2, w_gu, b_gu=None, act=GLU_SILU, gu=None, h=None, save=True
     elif gu is not None:
         raise ValueError("gu given with save=False")
     h = _out(h, "h", (M, F2 // 2), y2, stream=stream, dev=dev)
-    wp, wn = _gemm_ws(M, F2, H, ws, split, y2.device, stream)
+    wp, wn = _gemm_ws(M, F2, H, ws, split, y2.device, stream, "enc_glu_workspace_bytes")
     _call("enc_glu_up_fwd", M, H, F2 // 2, act, _ptr(y2), _ptr(w_gu), _ptr(b_gu), _ptr(gu), _ptr(h), wp, wn,
           _stream(stream))
     return gu, h
@@ -935,7 +944,7 @@ def enc_glu_down_bwd_data(dout, w_2, gu, act=GLU_SILU, dgu=None, ws=None, split=
     _check(w_2, "w_2", (H, F), dev=dev)
     _check(gu, "gu", (M, 2 * F), dev=dev)
     dgu = _out(dgu, "dgu", (M, 2 * F), dout, stream=stream, dev=dev)
-    wp, wn = _gemm_ws(M, F, H, ws, split, dout.device, stream)
+    wp, wn = _gemm_ws(M, F, H, ws, split, dout.device, stream, "enc_glu_workspace_bytes")
     _call("enc_glu_down_bwd_data", M, F, H, act, _ptr(dout), _ptr(w_2), _ptr(gu), _ptr(dgu), wp, wn, _stream(stream))
     return dgu
 
@@ -949,7 +958,7 @@ def enc_glu_up_bwd_data(dgu, w_gu, dy2=None, ws=None, split=True, stream=None):
     _check(dgu, "dgu", (M, F2), dev=dev)
     _check(w_gu, "w_gu", (F2, H), dev=dev)
     dy2 = _out(dy2, "dy2", (M, H), dgu, stream=stream, dev=dev)
-    wp, wn = _gemm_ws(M, H, F2, ws, split, dgu.device, stream)
+    wp, wn = _gemm_ws(M, H, F2, ws, split, dgu.device, stream, "enc_glu_workspace_bytes")
     _call("enc_glu_up_bwd_data", M, H, F2 // 2, _ptr(dgu), _ptr(w_gu), _ptr(dy2), wp, wn, _stream(stream))
     return dy2
 

@@ -734,6 +734,15 @@ int enc_qkv_bwd_data_add(int M, int H, int A, const enc_bf16 *dqkv, const enc_bf
   return launched(fn);
 }
 
+int enc_glu_workspace_bytes(int M, int N, int K, size_t *bytes) {
+  const char *fn = "enc_glu_workspace_bytes";
+  int r = linear_dims(fn, M, {N, K});
+  if (r) return r;
+  if (!bytes) return fail(ENC_ERR_INVALID, "%s: bytes is NULL", fn);
+  *bytes = glu_ws_bytes(M, N, K);
+  return ok();
+}
+
 int enc_linear_workspace_bytes(int M, int N, int K, size_t *bytes) {
   const char *fn = "enc_linear_workspace_bytes";
   int r = linear_dims(fn, M, {N, K});

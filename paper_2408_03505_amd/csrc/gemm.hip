@@ -84,7 +84,11 @@ constexpr bool has_activation(Epi e) {
 // 64-wide k-step.  The gated feed-forward block's do: its width is a fraction of
 // the model's (8/3, say), often no multiple of 64.  (The others keep the
 // register-staged kernel there, and with it their results.)
-constexpr bool takes_tail(Epi e) { return e == Epi::kGlu || e == Epi::kGluGrad || e == Epi::kPlainTail; }
+constexpr bool takes_tail(Epi e) {
+  return e == Epi::kGlu || e == Epi::kGluGrad || e == Epi::kPlainTail || e == Epi::kF32Tail;
+}
+// Whether it stores fp32 results or partials.
+constexpr bool is_f32(Epi e) { return e == Epi::kF32 || e == Epi::kF32Tail; }
 
 // Logical tile for this workgroup.  MI355X dispatches workgroup i to XCD
 // i % 8.  When the tile grid splits evenly, the XCDs form two halves along M,
@@ -210,7 +214,7 @@ __device__ __forceinline__ void store_tile(const GemmArgs &p, const f32x16_t (&a
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = acc[i][j][q * 4 + e];
         const size_t off = static_cast<size_t>(m) * p.ldy + nb;
-        if constexpr (EPI == Epi::kF32) {
+        if constexpr (is_f32(EPI)) {
           f32x4_t w{v[0], v[1], v[2], v[3]};
           if (p.accumulate) w += *reinterpret_cast<const f32x4_t *>(p.Wf + off);
           *reinterpret_cast<f32x4_t *>(p.Wf + off) = w;
@@ -365,7 +369,7 @@ __device__ __forceinline__ void store_tile_lds(const GemmArgs &p, const f32x4_t 
       }
     }
     __syncthreads();
-    if constexpr (EPI == Epi::kF32) {
+    if constexpr (is_f32(EPI)) {
       constexpr int PER_ROW = BN / 4;
       for (int it = tid; it < kEpiRows * PER_ROW; it += NT) {
         const int r = it / PER_ROW, cc = (it % PER_ROW) * 4;
@@ -969,8 +973,8 @@ __global__ __launch_bounds__(512, 1) void gemm_half_kernel(GemmArgs p, uint32_t 
     }
   };
 
-  // a contraction that is no multiple of 64 (not split): the last k-step's columns
-  const int tail = TAIL ? p.K % BK : 0;
+  // a contraction that is no multiple of 64 (its last split): the last k-step's columns
+  const int tail = TAIL ? klen % BK : 0;
   auto end_columns = [&] {
     la.end_columns(tail, wid, lane);
     lb.end_columns(tail, wid, lane);
@@ -1280,7 +1284,7 @@ __global__ __launch_bounds__(512, 2 * WGS) void gemm_ring_kernel(GemmArgs p, uin
   constexpr std::integral_constant<int, 0> c0{};
   constexpr std::integral_constant<int, 1> c1{};
   constexpr bool TAIL = takes_tail(EPI);
-  const int tail = TAIL ? p.K % BK : 0;  // a contraction that is no multiple of 64 (not split)
+  const int tail = TAIL ? klen % BK : 0;  // a contraction that is no multiple of 64 (its last split)
   // loads of k-step k; LAST: it may be the last one
   auto issue = [&](auto st, auto last, int k) {
     if constexpr (TAIL && decltype(last)::value) {
@@ -1416,7 +1420,7 @@ bool launch_ring_cfg(const GemmArgs &a, uint32_t a_bytes, uint32_t b_bytes, hipS
 template <bool AT, bool BT, Epi EPI>
 bool launch_lds(const GemmArgs &a, hipStream_t s, TileShape t) {
   constexpr bool gelu = has_activation(EPI);
-  constexpr GemmLayout row = !AT && EPI == Epi::kF32 ? kSplit : gemm_layout(AT, BT, gelu);
+  constexpr GemmLayout row = !AT && is_f32(EPI) ? kSplit : gemm_layout(AT, BT, gelu);
   if (!lds_fits(a.M, a.N, a.K, a.lda, a.ldb, AT, BT, takes_tail(EPI))) return false;
   // operand extents (bytes) bound the buffer loads
   const uint32_t ab = static_cast<uint32_t>(static_cast<uint64_t>(AT ? a.K : a.M) * a.lda * 2);
@@ -1570,8 +1574,9 @@ __global__ __launch_bounds__(256) void splitk_glu_kernel(const float *__restrict
 // missing or too small.
 template <bool BT, Epi EPI>
 bool launch_split(const GemmArgs &a, void *ws, size_t ws_bytes, hipStream_t s) {
-  const SplitPlan sp = gemm_split_plan(a.M, a.N, a.K);
-  if (sp.splits <= 1 || ws == nullptr || ws_bytes < gemm_ws_bytes(a.M, a.N, a.K) ||
+  constexpr bool kTail = takes_tail(EPI);
+  const SplitPlan sp = kTail ? glu_split_plan(a.M, a.N, a.K, ws_bytes) : gemm_split_plan(a.M, a.N, a.K);
+  if (sp.splits <= 1 || ws == nullptr || (!kTail && ws_bytes < gemm_ws_bytes(a.M, a.N, a.K)) ||
       a.ldy != (EPI == Epi::kGluGrad ? 2 * a.N : a.N) || a.N % 8)
     return false;
   GemmArgs b = a;
@@ -1582,7 +1587,13 @@ bool launch_split(const GemmArgs &a, void *ws, size_t ws_bytes, hipStream_t s) {
   b.Wf = static_cast<float *>(ws);
   b.db = nullptr;
   b.accumulate = 0;
-  if (!launch_lds<false, BT, Epi::kF32>(b, s, sp.tile)) return false;
+  if constexpr (kTail) {
+    const bool whole = a.K % 64 == 0;
+    if (!(whole ? launch_lds<false, BT, Epi::kF32>(b, s, sp.tile) : launch_lds<false, BT, Epi::kF32Tail>(b, s, sp.tile)))
+      return false;
+  } else {
+    if (!launch_lds<false, BT, Epi::kF32>(b, s, sp.tile)) return false;
+  }
   if constexpr (EPI == Epi::kGlu || EPI == Epi::kGluGrad) {
     const int F = EPI == Epi::kGlu ? a.N / 2 : a.N;
     const long f8 = static_cast<long>(a.M) * F / 8;
@@ -1591,7 +1602,8 @@ bool launch_split(const GemmArgs &a, void *ws, size_t ws_bytes, hipStream_t s) {
   } else {
     const long n8 = static_cast<long>(a.M) * a.N / 8;
     const int blocks = static_cast<int>(std::min<long>((n8 + 255) / 256, 2048));
-    hipLaunchKernelGGL((splitk_epilogue_kernel<EPI>), dim3(blocks), dim3(256), 0, s, b.Wf, sp.splits, b.split_stride,
+    constexpr Epi kEnd = EPI == Epi::kPlainTail ? Epi::kPlain : EPI;
+    hipLaunchKernelGGL((splitk_epilogue_kernel<kEnd>), dim3(blocks), dim3(256), 0, s, b.Wf, sp.splits, b.split_stride,
                        a.M, a.N, a.bias, a.R, a.Y, a.Y2);
   }
   return true;
@@ -1630,7 +1642,8 @@ bool launch_gemm_dgrad(const GemmArgs &a, Epi epi, void *ws, size_t ws_bytes, hi
     case Epi::kGluGrad: return dgrad_any<Epi::kGluGrad>(a, ws, ws_bytes, s);
     case Epi::kPlainTail:
       // (a contraction of whole k-steps is the plain product, split or not)
-      return (a.K % 64 != 0 && launch_lds<false, true, Epi::kPlainTail>(a, s)) ||
+      return (a.K % 64 != 0 && (launch_split<true, Epi::kPlainTail>(a, ws, ws_bytes, s) ||
+                                launch_lds<false, true, Epi::kPlainTail>(a, s))) ||
              dgrad_any<Epi::kPlain>(a, ws, ws_bytes, s);
     default: return false;
   }

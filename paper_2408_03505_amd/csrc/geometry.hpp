@@ -281,6 +281,20 @@ inline SplitPlan gemm_split_plan(int M, int N, int K) {
   return {1, K, choose_tile(M, N, K, kFwd)};
 }
 
+// The gated feed-forward block's products split where the contraction is no multiple
+// of 64, too (the last split's last k-step ends where it does), into no more parts
+// than the workspace holds.
+inline SplitPlan glu_split_plan(int M, int N, int K, size_t ws_bytes) {
+  SplitPlan sp = gemm_split_plan(M, N, (K + 63) / 64 * 64);
+  const size_t room = ws_bytes / (static_cast<size_t>(M) * N * sizeof(float));
+  if (room < static_cast<size_t>(sp.splits)) {
+    const int parts = std::max(static_cast<int>(room), 1);
+    sp.k_chunk = ((K + parts - 1) / parts + 63) / 64 * 64;
+    sp.splits = (K + sp.k_chunk - 1) / sp.k_chunk;
+  }
+  return sp;
+}
+
 // Whether the direct-to-LDS kernels take a product (operands A(m, k) and
 // B(n, k) with leading dimensions lda, ldb; AT / BT: stored k-major):
 // contiguous-k operands need whole 64-wide k-steps (unless the kernel ends the
@@ -339,6 +353,8 @@ inline size_t gemm_ws_bytes(int M, int N, int K) {
   const SplitPlan sp = gemm_split_plan(M, N, K);
   return sp.splits > 1 ? ws_round256(static_cast<size_t>(sp.splits) * M * N * sizeof(float)) : 0;
 }
+
+inline size_t glu_ws_bytes(int M, int N, int K) { return gemm_ws_bytes(M, N, (K + 63) / 64 * 64); }
 
 // Workspace of a split weight gradient: the fp32 partials of dW [S][M][N]
 // and of db [S][M], each 256-byte aligned; 0 when the plan does not split.

@@ -58,6 +58,7 @@ enum class Epi : int {
   // and dh = acc, Y[m, 2F] = [dh u act'(g) | dh act(g)]      (bf16 out)
   kGluGrad = 8,
   kPlainTail = 9,  // kPlain, over a contraction that need not be a multiple of 64
+  kF32Tail = 10,   // kF32 of such a contraction (partials of a split)
 };
 
 struct GemmArgs {

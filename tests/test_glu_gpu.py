@@ -179,6 +179,31 @@ def test_split_contractions(M, H, F, act):
 
 
 @gpu
+@pytest.mark.parametrize("M,H,F", [(1, 1032, 264), (17, 1288, 1000), (33, 2040, 2056), (64, 1304, 3416), (200, 1096, 520)])
+def test_splits_that_end_inside_a_step(M, H, F):
+    """Contractions over H and 2F that are no multiple of 64, split, with every
+    workspace down to none."""
+    assert B.linear_workspace_bytes(M, 2 * F, H) == 0 and B.glu_workspace_bytes(M, 2 * F, H) > 0
+    for split in (True, False):
+        _forward(M, H, F, "silu", split=split)
+        _backward(M, H, F, "gelu", split=split)
+        _up_backward(M, H, F, split=split)
+    for N, K, call in ((F, H, lambda ws: B.enc_glu_down_bwd_data(dout, w2, gu, ws=ws)),
+                       (H, 2 * F, lambda ws: B.enc_glu_up_bwd_data(gu, w, ws=ws))):
+        dout, w2, gu = cuda(random_bf16((M, H), 1)), cuda(random_bf16((H, F), 2)), cuda(random_bf16((M, 2 * F), 3))
+        w = cuda(random_bf16((2 * F, H), 4))
+        whole = f64(call(None))
+        need, part = B.glu_workspace_bytes(M, N, K), 4 * M * N
+        # a part less than needed each time: fp32 sums in another order, then one rounding
+        for size in range(need, 0, -part):
+            ws = torch.full((size + 64,), 0x7f, dtype=torch.uint8, device="cuda")
+            announce(f"M={M} N={N} K={K} workspace of {size} of {need} bytes")
+            got = f64(call(ws[:size]))
+            assert np.abs(got - whole).max() <= 2 ** -7 * np.abs(whole).max()
+            assert (ws[size:] == 0x7f).all()
+
+
+@gpu
 def test_extreme_gates():
     """Gates far out on both sides: the activation is g or 0, never NaN."""
     M, H, F = 64, 64, 64

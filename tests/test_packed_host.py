@@ -86,6 +86,19 @@ def test_plan_sizes():
     assert _st("enc_attn_packed_bwd_workspace_bytes", 4, 4, None) == INV
 
 
+def test_glu_workspace_sizes():
+    # the other products' where the contraction is a multiple of 64, and never less
+    for M, N, K in ((1, 512, 1280), (64, 3416, 1280), (200, 768, 6144), (5003, 1280, 6848), (2048, 6144, 4096)):
+        assert B.glu_workspace_bytes(M, N, K) == B.linear_workspace_bytes(M, N, K)
+        assert B.linear_workspace_bytes(M, N, K - 8) == 0
+        assert B.glu_workspace_bytes(M, N, K - 8) == B.linear_workspace_bytes(M, N, K)
+    assert B.glu_workspace_bytes(64, 3416, 1272) > 0
+    n = ctypes.c_size_t()
+    assert _st("enc_glu_workspace_bytes", 0, 8, 8, ctypes.byref(n)) == INV
+    assert _st("enc_glu_workspace_bytes", 8, 12, 8, ctypes.byref(n)) == UNS
+    assert _st("enc_glu_workspace_bytes", 8, 8, 8, None) == INV
+
+
 @no_gpu_only
 def test_attention_refusals():
     need = B.packed_plan_bytes(64, 3)
