@@ -337,12 +337,20 @@ inline GemmPlan gemm_plan(int M, int N, int K, int lda, int ldb, bool AT, bool B
 
 // Whether a gated feed-forward block's forward runs the kernel for few tokens.
 // That kernel reads the tokens' rows once per 8 columns of F, which costs M / 16
-// of the weights' bytes again, from the caches: nothing where its single launch
-// is the gain, a quarter of the time of a large weight.  At 16 tokens, us, against
-// the tiled product: 1280 x 3416 9.1 / 16.2, 6144 x 2048 18.4 / 21.8, but 6144 x
-// 16384 115 / 77-95; at 4 tokens there 79 / 78-95.
+// of the weights' bytes again, from the caches.  Up to four tokens it takes as long
+// as the tiled product or less at any size; with more it gains where that has too
+// few tiles and would split a long contraction over two launches, or where a call's
+// latency is all there is.  us with the weight in the caches / from HBM, against the
+// tiled product:
+//   1280 x 3416   16 tokens 7.2 / 8.4, 12.8 / 15.9; 32 tokens 10.1 / 12.4, 13.0 / 16.1
+//   4096 x 4096   16 tokens 17.2 / 20.2, 22.4 / 24.6; 32 tokens 25.3 / 30.1, 17.6 / 19.9
+//   1152 x 4304 (not split)  4 tokens 7.1 / 8.2, 7.4 / 8.4; 8 tokens 7.6 / 8.9, 7.0 / 8.4
+//   2048 x 8192 (not split)  4 tokens 13.1 / 14.9, 12.3 / 17.1; 8 tokens 14.4 / 16.9, 12.3 / 17.0
+//   768 x 2048 (not split)   32 tokens 6.0 / 5.9, 6.9 / 6.4
 inline bool glu_few_tokens(int M, int F, int K) {
-  return M <= 4 || (M <= 16 && 2ll * F * K <= (1ll << 25));
+  if (M <= 4 || M > 32) return M <= 4;
+  const bool few_tiles = K >= 2 * kMinSplitTokens && tiles_256(M, 2 * F) <= 32;
+  return 2ll * F * K <= (few_tiles ? (M <= 16 ? 1ll << 25 : 1ll << 24) : 1ll << 22);
 }
 
 inline size_t ws_round256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }

@@ -1,5 +1,5 @@
 // A gated feed-forward block's up-projections, activation and product for a few
-// tokens (serving): [g | u] = y Wgu^T + b, h = act(g) u, of up to 16 rows.
+// tokens (serving): [g | u] = y Wgu^T + b, h = act(g) u, of up to 32 rows.
 //
 // Bound by reading the weights once.  Each workgroup takes 8 columns of F: their
 // gate and up-projection rows are the 16 rows of the A operand of
@@ -9,8 +9,8 @@
 // operand comes from the caches.  The waves' fp32 sums are added in LDS in wave
 // order, then bias, activation and product follow: one launch, no workspace.
 // One token, us (TB/s of weights), against the tiled product and its split's
-// second launch: 1280 x 3416 6.6 (2.7) / 15.7, 6144 x 2048 12.9 (3.9) / 21.1,
-// 6144 x 16384 72 (5.6) / 78-95.
+// second launch: 1280 x 3416 6.0 (2.9) / 15.4, 6144 x 2048 12.0 (4.2) / 20.5,
+// 6144 x 16384 71 (5.7) / 75-92.
 #include "common.hpp"
 #include "gate.hpp"
 #include "kernels.hpp"
@@ -21,21 +21,24 @@ namespace {
 
 constexpr int kCols = 8, kWaves = 8, kAhead = 4;
 
+template <int NB>  // 16 tokens each
 __global__ __launch_bounds__(64 * kWaves) void glu_small_kernel(int M, int F, int K, int act,
                                                                 const bf16_t *__restrict__ y,
                                                                 const bf16_t *__restrict__ w,
                                                                 const bf16_t *__restrict__ bias,
                                                                 bf16_t *__restrict__ gu, bf16_t *__restrict__ h) {
-  __shared__ f32x4_t part[kWaves][64];
+  __shared__ f32x4_t part[kWaves][NB][64];
   const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
   const int j0 = blockIdx.x * kCols, r = lane & 15, kl = (lane >> 4) * 8;
   // (F is a multiple of 8: every column of the workgroup exists)
   const bf16_t *wr = w + static_cast<size_t>(j0 + (r & 7) + (r >= 8 ? F : 0)) * K;
   const u32x4_t zero{0u, 0u, 0u, 0u};
   const int steps = (K + 63) / 64;
-  f32x4_t acc{0.f, 0.f, 0.f, 0.f};
+  f32x4_t acc[NB];
+#pragma unroll
+  for (int n = 0; n < NB; ++n) acc[n] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   for (int s0 = wid; s0 < steps; s0 += kWaves * kAhead) {
-    u32x4_t a[kAhead][2], b[kAhead][2];
+    u32x4_t a[kAhead][2], b[kAhead][2][NB];
 #pragma unroll
     for (int i = 0; i < kAhead; ++i)
 #pragma unroll
@@ -43,22 +46,28 @@ __global__ __launch_bounds__(64 * kWaves) void glu_small_kernel(int M, int F, in
         const int k = (s0 + i * kWaves) * 64 + e * 32 + kl;
         const bool in = k < K;  // (K is a multiple of 8)
         a[i][e] = in ? ldg16(wr + k) : zero;
-        b[i][e] = in && r < M ? ldg16(y + static_cast<size_t>(r) * K + k) : zero;
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+          b[i][e][n] = in && 16 * n + r < M ? ldg16(y + static_cast<size_t>(16 * n + r) * K + k) : zero;
       }
 #pragma unroll
     for (int i = 0; i < kAhead; ++i)
 #pragma unroll
-      for (int e = 0; e < 2; ++e) acc = mfma16(as_bf16x8(a[i][e]), as_bf16x8(b[i][e]), acc);
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int n = 0; n < NB; ++n) acc[n] = mfma16(as_bf16x8(a[i][e]), as_bf16x8(b[i][e][n]), acc[n]);
   }
-  part[wid][lane] = acc;
+#pragma unroll
+  for (int n = 0; n < NB; ++n) part[wid][n][lane] = acc[n];
   __syncthreads();
   // lanes 0..31 of a result hold four gates of token lane % 16, lanes 32..63
   // the same columns' up-projections
-  if (threadIdx.x < 32) {
-    f32x4_t gs = part[0][lane], us = part[0][lane + 32];
+  if (threadIdx.x < 32 * NB) {
+    const int n = lane >> 5, l = lane & 31;
+    f32x4_t gs = part[0][n][l], us = part[0][n][l + 32];
 #pragma unroll
-    for (int s = 1; s < kWaves; ++s) gs += part[s][lane], us += part[s][lane + 32];
-    const int m = r, j = j0 + (lane >> 4) * 4;
+    for (int s = 1; s < kWaves; ++s) gs += part[s][n][l], us += part[s][n][l + 32];
+    const int m = 16 * n + r, j = j0 + (l >> 4) * 4;
     if (m >= M) return;
     float gv[4], uv[4];
 #pragma unroll
@@ -81,7 +90,8 @@ __global__ __launch_bounds__(64 * kWaves) void glu_small_kernel(int M, int F, in
 
 bool launch_glu_small(int M, int F, int K, int act, const bf16_t *y, const bf16_t *w, const bf16_t *bias, bf16_t *gu,
                       bf16_t *h, hipStream_t s) {
-  hipLaunchKernelGGL(glu_small_kernel, dim3(F / kCols), dim3(64 * kWaves), 0, s, M, F, K, act, y, w, bias, gu, h);
+  hipLaunchKernelGGL(M <= 16 ? glu_small_kernel<1> : glu_small_kernel<2>, dim3(F / kCols), dim3(64 * kWaves), 0, s, M, F,
+                     K, act, y, w, bias, gu, h);
   return true;
 }
 

@@ -99,7 +99,7 @@ bool launch_gemm_dgrad(const GemmArgs &a, Epi epi, void *ws, size_t ws_bytes, hi
 // ws = nullptr never splits.
 bool launch_gemm_wgrad(const GemmArgs &a, void *ws, size_t ws_bytes, hipStream_t s, FinishJobs *defer = nullptr);
 
-// ---- Gated feed-forward for up to 16 tokens: [g | u] = y Wgu^T + b (K columns),
+// ---- Gated feed-forward for up to 32 tokens: [g | u] = y Wgu^T + b (K columns),
 // h = act(g) u; gu and bias may be null.
 bool launch_glu_small(int M, int F, int K, int act, const bf16_t *y, const bf16_t *w, const bf16_t *bias, bf16_t *gu,
                       bf16_t *h, hipStream_t s);

@@ -129,7 +129,7 @@ def test_contractions_that_end_inside_a_step(steps, more):
 
 @gpu
 @pytest.mark.parametrize("act", ["silu", "gelu"])
-@pytest.mark.parametrize("M", [1, 2, 4, 5, 15, 16, 17])
+@pytest.mark.parametrize("M", [1, 2, 4, 5, 15, 16, 17, 24, 32, 33])
 def test_few_tokens(M, act):
     """Sizes on both sides of the rule that picks the kernel for few tokens."""
     for H, F in ((8, 8), (72, 40), (512, 24), (1288, 344), (2048, 520), (2056, 8200)):
