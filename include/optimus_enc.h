@@ -538,9 +538,9 @@ enum enc_glu_act {
   ENC_GLU_GELU = 1  /* act(g) = g Phi(g) (exact erf form) */
 };
 
-/* The workspace that the block's products (output [M, N], contraction K) make use
- * of: enc_linear_workspace_bytes where K is a multiple of 64, and where it is not
- * what splitting it takes.  A smaller one splits it into fewer parts. */
+/* The most workspace that the block's products (output [M, N], contraction K) make
+ * use of: enc_linear_workspace_bytes where K is a multiple of 64, and where it is
+ * not what splitting it takes.  A smaller one splits it into fewer parts. */
 int enc_glu_workspace_bytes(int M, int N, int K, size_t *bytes);
 /* [Gated block step: both up-projections, the activation and the product]
  * y2 [M, H]; b_gu [2F] or NULL; h [M, F] bf16, from g and u in fp32; gu

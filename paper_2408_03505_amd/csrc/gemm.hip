@@ -1575,7 +1575,8 @@ __global__ __launch_bounds__(256) void splitk_glu_kernel(const float *__restrict
 template <bool BT, Epi EPI>
 bool launch_split(const GemmArgs &a, void *ws, size_t ws_bytes, hipStream_t s) {
   constexpr bool kTail = takes_tail(EPI);
-  const SplitPlan sp = kTail ? glu_split_plan(a.M, a.N, a.K, ws_bytes) : gemm_split_plan(a.M, a.N, a.K);
+  constexpr GemmLayout row = gemm_layout(false, BT, has_activation(EPI));
+  const SplitPlan sp = kTail ? glu_split_plan(a.M, a.N, a.K, ws_bytes, row) : gemm_split_plan(a.M, a.N, a.K);
   if (sp.splits <= 1 || ws == nullptr || (!kTail && ws_bytes < gemm_ws_bytes(a.M, a.N, a.K)) ||
       a.ldy != (EPI == Epi::kGluGrad ? 2 * a.N : a.N) || a.N % 8)
     return false;
@@ -1641,10 +1642,10 @@ bool launch_gemm_dgrad(const GemmArgs &a, Epi epi, void *ws, size_t ws_bytes, hi
     case Epi::kResid: return dgrad_any<Epi::kResid>(a, ws, ws_bytes, s);
     case Epi::kGluGrad: return dgrad_any<Epi::kGluGrad>(a, ws, ws_bytes, s);
     case Epi::kPlainTail:
-      // (a contraction of whole k-steps is the plain product, split or not)
-      return (a.K % 64 != 0 && (launch_split<true, Epi::kPlainTail>(a, ws, ws_bytes, s) ||
-                                launch_lds<false, true, Epi::kPlainTail>(a, s))) ||
-             dgrad_any<Epi::kPlain>(a, ws, ws_bytes, s);
+      // (a contraction of whole k-steps not split is the plain product)
+      return launch_split<true, Epi::kPlainTail>(a, ws, ws_bytes, s) ||
+             (a.K % 64 != 0 ? launch_lds<false, true, Epi::kPlainTail>(a, s) : launch_lds<false, true, Epi::kPlain>(a, s)) ||
+             launch_any<false, true, Epi::kPlain>(a, s);
     default: return false;
   }
 }

@@ -234,6 +234,11 @@ inline int wgrad_max_chunk(int M, int N, int K) {
   return ((K + s - 1) / s + 63) / 64 * 64;
 }
 
+// The second kernel's traffic (us): s partials read, one output written.
+inline float split_sum_us(int M, int N, int s) {
+  return static_cast<float>(s + 1) * static_cast<float>(M) * static_cast<float>(N) * (4.f / 4.5e6f);
+}
+
 inline SplitPlan best_split(int M, int N, int K, GemmLayout l) {
   SplitPlan best{1, K, {0, 0}};
   float best_us = 0.f;
@@ -248,8 +253,7 @@ inline SplitPlan best_split(int M, int N, int K, GemmLayout l) {
       if (small && n * s <= 256) continue;
       const int kc = ((K + s - 1) / s + 63) / 64 * 64;
       if ((K + kc - 1) / kc != s || kc > max_chunk) continue;
-      const float us = gemm_cost(t, row, n * s, kc / 64) +
-                       static_cast<float>(s + 1) * static_cast<float>(M) * static_cast<float>(N) * (4.f / 4.5e6f);
+      const float us = gemm_cost(t, row, n * s, kc / 64) + split_sum_us(M, N, s);
       if (best.splits == 1 || us < best_us) {
         best_us = us;
         best = {s, kc, {t.bm, t.bn}};
@@ -283,9 +287,16 @@ inline SplitPlan gemm_split_plan(int M, int N, int K) {
 
 // The gated feed-forward block's products split where the contraction is no multiple
 // of 64, too (the last split's last k-step ends where it does), into no more parts
-// than the workspace holds.
-inline SplitPlan glu_split_plan(int M, int N, int K, size_t ws_bytes) {
+// than the workspace holds, and only where the cost model has the split and its
+// second launch (4 us) ahead of the product in one: l is that one's row.
+inline SplitPlan glu_split_plan(int M, int N, int K, size_t ws_bytes, GemmLayout l) {
   SplitPlan sp = gemm_split_plan(M, N, (K + 63) / 64 * 64);
+  if (sp.splits == 1) return sp;
+  for (const TileCost &t : kTiles)
+    if (t.bm == sp.tile.bm && t.bn == sp.tile.bn &&
+        gemm_cost(t, kSplit, tile_count(t, M, N) * sp.splits, sp.k_chunk / 64) + split_sum_us(M, N, sp.splits) + 4.f >=
+            pick_tile(M, N, K, l).us)
+      return {1, K, sp.tile};
   const size_t room = ws_bytes / (static_cast<size_t>(M) * N * sizeof(float));
   if (room < static_cast<size_t>(sp.splits)) {
     const int parts = std::max(static_cast<int>(room), 1);
@@ -338,18 +349,19 @@ inline GemmPlan gemm_plan(int M, int N, int K, int lda, int ldb, bool AT, bool B
 // Whether a gated feed-forward block's forward runs the kernel for few tokens.
 // That kernel reads the tokens' rows once per 8 columns of F, which costs M / 16
 // of the weights' bytes again, from the caches.  Up to four tokens it takes as long
-// as the tiled product or less at any size; with more it gains where that has too
-// few tiles and would split a long contraction over two launches, or where a call's
-// latency is all there is.  us with the weight in the caches / from HBM, against the
-// tiled product:
-//   1280 x 3416   16 tokens 7.2 / 8.4, 12.8 / 15.9; 32 tokens 10.1 / 12.4, 13.0 / 16.1
+// as the tiled product or less at any size; with more it gains where that has few
+// tiles and a long contraction, which it walks in turn or splits over two launches,
+// or where a call's latency is all there is.  us with the weight in the caches /
+// from HBM, against the tiled product:
+//   4096 x 1024   16 tokens 9.8 / 10.6, 16.3 / 19.7; 32 tokens 13.7 / 14.6, 17.0 / 20.1
 //   4096 x 4096   16 tokens 17.2 / 20.2, 22.4 / 24.6; 32 tokens 25.3 / 30.1, 17.6 / 19.9
-//   1152 x 4304 (not split)  4 tokens 7.1 / 8.2, 7.4 / 8.4; 8 tokens 7.6 / 8.9, 7.0 / 8.4
-//   2048 x 8192 (not split)  4 tokens 13.1 / 14.9, 12.3 / 17.1; 8 tokens 14.4 / 16.9, 12.3 / 17.0
-//   768 x 2048 (not split)   32 tokens 6.0 / 5.9, 6.9 / 6.4
+//   1280 x 3416   8 tokens 6.3 / 7.1, 32 tokens 10.1 / 12.4, against 7.4 in the caches
+//   1152 x 4304   4 tokens 7.1 / 8.2, 7.4 / 8.4; 8 tokens 7.6 / 8.9, 7.0 / 8.4
+//   2048 x 8192   4 tokens 13.1 / 14.9, 12.3 / 17.1; 8 tokens 14.4 / 16.9, 12.3 / 17.0
+//   768 x 2048    32 tokens 6.0 / 5.9, 6.9 / 6.4
 inline bool glu_few_tokens(int M, int F, int K) {
   if (M <= 4 || M > 32) return M <= 4;
-  const bool few_tiles = K >= 2 * kMinSplitTokens && tiles_256(M, 2 * F) <= 32;
+  const bool few_tiles = K >= (M <= 16 ? 1024 : 2048) && tiles_256(M, 2 * F) <= 32;
   return 2ll * F * K <= (few_tiles ? (M <= 16 ? 1ll << 25 : 1ll << 24) : 1ll << 22);
 }
 

@@ -179,6 +179,23 @@ def test_split_contractions(M, H, F, act):
 
 
 @gpu
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("M,H,F", [(33, 4096, 1024), (40, 4104, 1000), (200, 6144, 264), (70, 6152, 2056)])
+def test_long_contractions_are_split(M, H, F, act):
+    """Contractions over H that the products with an activation split (short ones they
+    take whole): the sums' order shows in some bits of the results."""
+    y, w, w2 = cuda(random_bf16((M, H), 1)), cuda(random_bf16((2 * F, H), 2)), cuda(random_bf16((H, F), 3))
+    gu = cuda(random_bf16((M, 2 * F), 4))
+    for call in (lambda split: B.enc_glu_up_fwd(y, w, act=ACTS[act], split=split)[1],
+                 lambda split: B.enc_glu_down_bwd_data(y, w2, gu, act=ACTS[act], split=split)):
+        assert not torch.equal(call(True), call(False))
+    for split in (True, False):
+        _forward(M, H, F, act, split=split)
+        _forward(M, H, F, act, bias=False, save=False, split=split)
+        _backward(M, H, F, act, split=split)
+
+
+@gpu
 @pytest.mark.parametrize("M,H,F", [(1, 1032, 264), (17, 1288, 1000), (33, 2040, 2056), (64, 1304, 3416), (200, 1096, 520)])
 def test_splits_that_end_inside_a_step(M, H, F):
     """Contractions over H and 2F that are no multiple of 64, split, with every
