@@ -498,7 +498,9 @@ int enc_rope_bwd(int M, int heads, int kv_heads, int head_dim, int sec_t, int se
  * of any head layout; it is built once per batch.  Its contents are the
  * library's own.  Offsets outside [0, tokens] are taken as the nearest bound
  * and a sequence that would end before it starts as empty; where sequences
- * overlap, results are undefined (nothing outside the tensors is touched). */
+ * overlap, results are undefined (nothing outside the tensors is touched).
+ * At most 11184810 tokens, the most that an attention call takes (one query and
+ * one key head of 64). */
 int enc_packed_plan_bytes(int tokens, int seqs, size_t *bytes);
 int enc_packed_plan(int tokens, int seqs, const int32_t *cu_seqlens, void *plan, size_t plan_bytes,
                     enc_stream_t stream);

@@ -83,6 +83,10 @@ constexpr long kMaxElems = 1L << 31;
 // head_dim is an int.
 constexpr int kMaxSeqs = 65536, kMaxHeads = 65536;
 
+// Rows of the narrowest qkv (a query, a key and a value head of 64) within kMaxElems:
+// more than these no attention call takes.
+constexpr int kMaxPackedTokens = static_cast<int>((kMaxElems - 1) / (3 * 64));
+
 // A launcher refused a shape that the argument checks accepted.  The checks
 // cover every refusal condition (check_cfg), so this is unreachable; if it
 // ever happens, kernels of the same call may already be enqueued, which is
@@ -1065,6 +1069,8 @@ int enc_packed_plan(int tokens, int seqs, const int32_t *cu_seqlens, void *plan,
   const char *fn = "enc_packed_plan";
   int r = packed_seqs(fn, tokens, seqs);
   if (r) return r;
+  if (tokens > kMaxPackedTokens)
+    return fail(ENC_ERR_UNSUPPORTED, "%s: more than %d tokens, which no attention call takes", fn, kMaxPackedTokens);
   PtrCheck c(fn);
   c.req(cu_seqlens, "cu_seqlens").req(plan, "plan");
   if (c.code) return c.code;

@@ -72,6 +72,12 @@ struct PackedPlan {
 
 inline int packed_slots(int tokens, int seqs) { return tokens / kPackedRows + seqs; }
 
+// Items of a sequence.
+constexpr int packed_tiles(int len) { return len / kPackedRows + (len % kPackedRows != 0); }
+static_assert(packed_tiles(0) == 0 && packed_tiles(1) == 1 && packed_tiles(kPackedRows) == 1 &&
+                  packed_tiles(kPackedRows + 1) == 2 && packed_tiles(0x7fffffff) == 0x7fffffff / kPackedRows + 1,
+              "items of a sequence of any length");
+
 inline size_t packed_plan_bytes(int tokens, int seqs) {
   const size_t b = sizeof(PackedItem) * (1 + static_cast<size_t>(tokens / kPackedRows) + seqs);
   return (b + 255) & ~static_cast<size_t>(255);

@@ -21,21 +21,19 @@ __device__ __forceinline__ void sequence(const int *cu, int i, int tokens, int &
   len = min(max(cu[i + 1], first), tokens) - first;
 }
 
-__device__ __forceinline__ int tiles_of(int len) { return (len + kPackedRows - 1) / kPackedRows; }
-
 __global__ __launch_bounds__(256) void packed_plan_kernel(int tokens, int seqs, int cap, const int *__restrict__ cu,
                                                           PackedPlan *__restrict__ plan) {
   __shared__ int tiles[256];
   const int tid = threadIdx.x, mine = blockIdx.x * 256 + tid;
   int first = 0, len = 0;
   if (mine < seqs) sequence(cu, mine, tokens, first, len);
-  const int t = tiles_of(len);
+  const int t = packed_tiles(len);
   long before = 0, total = 0;
   for (int j0 = 0; j0 < seqs; j0 += 256) {
     int f, l = 0;
     if (j0 + tid < seqs) sequence(cu, j0 + tid, tokens, f, l);
     __syncthreads();
-    tiles[tid] = tiles_of(l);
+    tiles[tid] = packed_tiles(l);
     __syncthreads();
     const int n = min(256, seqs - j0);  // (the others of the 256 have no tiles)
     for (int j = 0; j < n; j += 8)

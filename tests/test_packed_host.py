@@ -74,6 +74,21 @@ def test_plan_refusals():
     assert _st("enc_packed_plan_bytes", 64, 65537, ctypes.byref(n)) == UNS
 
 
+@no_gpu_only
+def test_plans_of_more_rows_than_attention_takes_are_refused():
+    most = (2 ** 31 - 1) // (3 * 64)  # rows of one query, key and value head of 64
+    narrow = list(FWD)
+    narrow[1], narrow[2], narrow[3] = 1, 1, 1
+    _bad("enc_attn_packed_fwd", narrow, [(0, most + 1, UNS), (0, 2 ** 31 - 1, UNS)])
+    for tokens in (most + 1, 2 ** 31 - 127, 2 ** 31 - 1):
+        _bad("enc_packed_plan", PLAN, [(0, tokens, UNS)])
+    if STUB:  # (the product library would launch on fake pointers)
+        for name, base in (("enc_packed_plan", PLAN), ("enc_attn_packed_fwd", narrow)):
+            args = list(base)
+            args[0] = most
+            assert _st(name, *args) == B.ENC_OK, B.lib().enc_last_error()
+
+
 def test_plan_sizes():
     # a header and one 16-byte item per 128 rows and sequence
     for tokens, seqs in ((1, 1), (128, 1), (129, 7), (100000, 40), (2 ** 31 - 1, 65536)):
