@@ -511,7 +511,8 @@ int enc_packed_plan(int tokens, int seqs, const int32_t *cu_seqlens, void *plan,
  * j <= i), o_i = sum_j P_ij v_j.  plan: enc_packed_plan for the same tokens
  * and seqs.  qkv: [tokens, (heads + 2 kv_heads) * head_dim]; o: [tokens,
  * heads * head_dim]; lse: [heads, tokens] fp32, natural log.  Rows of no
- * sequence keep what o and lse held.  (With causal = 1, a non-finite value of a
+ * sequence keep what o and lse held.  A logit of -inf weighs nothing; a query
+ * that sees no other has o = NaN.  (With causal = 1, a non-finite value of a
  * later token still reaches the queries before it in the same 32 tokens of its
  * sequence, counted from its first, as 0 times it.) */
 int enc_attn_packed_fwd(int tokens, int seqs, int heads, int kv_heads, int head_dim, int causal, const void *plan,

@@ -34,6 +34,7 @@
 // 147 MB, backward 97 for 441).  Figures beside the kernels are medians of a kernel
 // trace; rates count 4, 6 and 8 flops per query, key and element of a head in the
 // forward, dQ (S, dP and dQ) and dK/dV (S, dP, dV and dK).
+#include <float.h>
 #include <math.h>
 
 #include <algorithm>
@@ -393,7 +394,10 @@ packed_fwd_kernel(PackedAttnArgs p) {
 
   Result<D> acc;
   acc.zero();
-  float m = -INFINITY, top = -INFINITY, l = 0.f;
+  // m starts below every scaled logit but finite: a logit of -inf then weighs
+  // exp2(-inf - m) = 0 also where the tiles so far hold no other (from m = -inf it
+  // would weigh NaN)
+  float m = -FLT_MAX, top = -INFINITY, l = 0.f;
   const float c = kLog2e / sqrtf(static_cast<float>(D));
 
   PackedReadsR<D, false> rd;
@@ -420,12 +424,13 @@ packed_fwd_kernel(PackedAttnArgs p) {
   // by more than kLazyRescale (log2 units; `top` is that in raw logits): O = acc / l
   // and lse = m + log2 l hold for any m.  ms is the maximum over the half of the
   // tile's keys that this lane holds, which is enough to see whether any moves.
-  // (Every query sees key 0, so m is finite from tile 0 on.)
+  // (It moves at the first logit above -inf: those lie above -FLT_MAX, which c < 1
+  // takes far above m's start; `top` stays -inf until then, as m's start / c does.)
   auto move_max = [&](float ms) {
     if (__any(ms > top)) {
       const float mt = max_halves(ms) * c;
       const float mn = mt > m + kLazyRescale ? mt : m;
-      const float alpha = exp2_hw(m - mn);  // 0 on the first tile (m = -inf), 1 where m stays
+      const float alpha = exp2_hw(m - mn);  // 0 at the first move, 1 where m stays
       m = mn;
       top = (mn + kLazyRescale) / c;
       l *= alpha;

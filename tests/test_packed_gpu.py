@@ -201,6 +201,46 @@ def test_attention_of_large_logits(d):
     within(dqkv, ref, bound)
 
 
+@pytest.mark.parametrize("low", [torch.finfo(BF).min, float("-inf")])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("heads,kv,d", [(2, 2, 64), (4, 1, 80), (2, 1, 128)])
+def test_leading_keys_with_logits_of_minus_infinity(heads, kv, d, causal, low):
+    """The first 72 keys' logits are -inf (beyond fp32, with the lowest bf16 value): for
+    every query after them two whole tiles and a part of one weigh nothing."""
+    T, lead = 150, 72
+    announce(f"packed attention heads={heads}/{kv} d={d} causal={causal} leading keys {low}")
+    qkv, do, _ = _attn_inputs([0, T], T, heads, kv, d, 23)
+    x = qkv.view(T, heads + 2 * kv, d)
+    x[:, :heads, 0] = 16.0
+    x[:lead, heads:heads + kv] = 0.0
+    x[:lead, heads:heads + kv, 0] = low
+    plan = _plan([0, T], T)
+    o, lse = B.enc_attn_packed_fwd(1, heads, kv, d, cuda(qkv), plan, causal)
+    v = f64(x)
+    rows = slice(lead, T) if causal else slice(0, T)  # (with causal the others see no finite logit)
+    seen = np.tril(np.ones((T, T), dtype=bool)) if causal else np.ones((T, T), dtype=bool)
+    seen[:, :lead] = False
+    for h in range(heads):
+        q, k, w = v[:, h], v[lead:, heads + h // (heads // kv)], v[lead:, heads + kv + h // (heads // kv)]
+        s = np.where(seen[:, lead:], q @ k.T / np.sqrt(d), -np.inf)[rows]
+        m = s.max(1, keepdims=True)
+        p = np.exp(s - m)
+        total = p.sum(1, keepdims=True)
+        p /= total
+        # the oracle's bounds, over the keys that weigh something
+        size = (np.abs(q[rows]) @ np.abs(k).T / np.sqrt(d)).max(1, keepdims=True)
+        ds = P.FP32 * ((d + 4) * size + 4 * np.abs(m) + 8)
+        ref, rlse = p @ w, (m + np.log(total))[:, 0]
+        bound = (P.BF16 + 2 * ds + 2 * (T + 16) * P.FP32) * (p @ np.abs(w)) + P.BF16 * np.abs(ref) * (1 + P.BF16)
+        within(o[rows, h * d:(h + 1) * d], ref, bound)
+        within(lse[h, rows], rlse, (2 * ds + (T + 16) * P.FP32)[:, 0] + 4 * P.FP32 * np.abs(rlse))
+    if causal or low == float("-inf"):  # (0 times -inf in the backward's products)
+        return
+    dqkv = B.enc_attn_packed_bwd(1, heads, kv, d, cuda(qkv), o, lse, cuda(do), plan)
+    got = f64(dqkv).reshape(T, heads + 2 * kv, d)
+    assert np.isfinite(got).all() and (got[:lead, heads:] == 0).all()
+
+
 @pytest.mark.parametrize("heads,kv,d", [(2, 2, 64), (4, 1, 80), (2, 1, 128)])
 def test_a_later_token_reaches_no_earlier_tile(heads, kv, d):
     """With causal attention, non-finite keys and values from token 200 on leave the
