@@ -566,6 +566,12 @@ int enc_glu_up_bwd_data(int M, int H, int F, const enc_bf16 *dgu, const enc_bf16
  * N = 2F, K = H, and its workspace. */
 int enc_glu_up_bwd_weight(int M, int H, int F, const enc_bf16 *dgu, const enc_bf16 *y2, float *dw_gu, float *db_gu,
                           int accumulate, void *ws, size_t ws_bytes, enc_stream_t stream);
+/* Launch plan of one of the first three, as enc_linear_plan gives it of the other
+ * products: the output tile (of the forward: of its 2F columns of [g | u]) and the
+ * number of contraction splits with a workspace of ws_bytes (0: none).  *tile_rows =
+ * *tile_cols = 0 where the forward runs the kernel for few tokens.  Host only. */
+enum enc_glu_product { ENC_GLU_UP_FWD = 0, ENC_GLU_DOWN_BWD_DATA = 1, ENC_GLU_UP_BWD_DATA = 2 };
+int enc_glu_plan(int product, int M, int H, int F, size_t ws_bytes, int *tile_rows, int *tile_cols, int *splits);
 
 /* ------------------------------------------------------------ whole encoder
  *

@@ -120,6 +120,7 @@ _SIGS = {
     "enc_glu_down_bwd_data": [_i, _i, _i, _i, _p, _p, _p, _p, _p, _sz, _p],
     "enc_glu_up_bwd_data": [_i, _i, _i, _p, _p, _p, _p, _sz, _p],
     "enc_glu_up_bwd_weight": [_i, _i, _i, _p, _p, _p, _p, _i, _p, _sz, _p],
+    "enc_glu_plan": [_i, _i, _i, _i, _sz, ctypes.POINTER(_i), ctypes.POINTER(_i), ctypes.POINTER(_i)],
     "enc_patch_embed_workspace_bytes": [_i, _i, _i, _i, _i, _i, _i, ctypes.POINTER(_sz)],
     "enc_patch_embed_fwd": [_i, _i, _i, _i, _i, _i, _i, _p, _p, _p, _p, _p, _p, _p, _p, _sz, _p],
     "enc_patch_embed_bwd": [_i, _i, _i, _i, _i, _i, _i, _p, _p, _p, _p, _p, _p, _i, _p, _sz, _p],
@@ -911,6 +912,21 @@ GLU_SILU, GLU_GELU = 0, 1
 
 def glu_workspace_bytes(M, N, K):
     return _ws_bytes("enc_glu_workspace_bytes", M, N, K)
+
+
+GLU_UP_FWD, GLU_DOWN_BWD_DATA, GLU_UP_BWD_DATA = 0, 1, 2
+
+
+def glu_plan(product, M, H, F, ws_bytes=None):
+    """(tile_rows, tile_cols, splits) of a gated block's product with a workspace of
+    ws_bytes (None: as large as it makes use of); tiles of 0 x 0 where the forward runs
+    the kernel for few tokens (host query, no device work)."""
+    if ws_bytes is None:
+        dims = {GLU_UP_FWD: (2 * F, H), GLU_DOWN_BWD_DATA: (F, H), GLU_UP_BWD_DATA: (H, 2 * F)}
+        ws_bytes = glu_workspace_bytes(M, *dims[product]) if product in dims else 0
+    r, c, sp = _i(), _i(), _i()
+    _call("enc_glu_plan", product, M, H, F, ws_bytes, ctypes.byref(r), ctypes.byref(c), ctypes.byref(sp))
+    return r.value, c.value, sp.value
 
 
 def enc_glu_up_fwd(y2, w_gu, b_gu=None, act=GLU_SILU, gu=None, h=None, save=True, ws=None, split=True, stream=None):

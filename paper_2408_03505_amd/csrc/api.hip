@@ -1178,6 +1178,27 @@ int enc_glu_up_bwd_weight(int M, int H, int F, const enc_bf16 *dgu, const enc_bf
   return enc_linear_bwd_weight(M, 2 * F, H, dgu, y2, dw_gu, db_gu, accumulate, ws, ws_bytes, stream);
 }
 
+int enc_glu_plan(int product, int M, int H, int F, size_t ws_bytes, int *tile_rows, int *tile_cols, int *splits) {
+  const char *fn = "enc_glu_plan";
+  int r = glu_dims(fn, M, H, F, ENC_GLU_SILU);
+  if (r) return r;
+  if (!tile_rows || !tile_cols || !splits) return fail(ENC_ERR_INVALID, "%s: an output pointer is NULL", fn);
+  // the geometry that glu_fwd, glu_dgrad and glu_up_dgrad build
+  GemmPlan pl{{0, 0}, 1};
+  switch (product) {
+    case ENC_GLU_UP_FWD:
+      if (!glu_few_tokens(M, F, H)) pl = glu_plan(M, 2 * F, H, H, H, kFwdGelu, ws_bytes);
+      break;
+    case ENC_GLU_DOWN_BWD_DATA: pl = glu_plan(M, F, H, H, F, kDgradGelu, ws_bytes); break;
+    case ENC_GLU_UP_BWD_DATA: pl = glu_plan(M, H, 2 * F, 2 * F, H, kDgrad, ws_bytes); break;
+    default: return fail(ENC_ERR_INVALID, "%s: unknown product %d", fn, product);
+  }
+  *tile_rows = pl.tile.bm;
+  *tile_cols = pl.tile.bn;
+  *splits = pl.splits;
+  return ok();
+}
+
 int enc_parallel_saved_layout(const enc_cfg_t *cfg, enc_psaved_layout_t *layout) {
   const char *fn = "enc_parallel_saved_layout";
   int r = check_cfg(fn, cfg);

@@ -371,6 +371,16 @@ inline bool glu_few_tokens(int M, int F, int K) {
   return 2ll * F * K <= (few_tiles ? (M <= 16 ? 1ll << 25 : 1ll << 24) : 1ll << 22);
 }
 
+// Output tile and parts of a gated feed-forward block's product as the launchers take
+// it with a workspace of ws_bytes (l: its row of the cost table; the contraction may
+// end inside a 64-wide step).
+inline GemmPlan glu_plan(int M, int N, int K, int lda, int ldb, GemmLayout l, size_t ws_bytes) {
+  if (!lds_fits(M, N, K, lda, ldb, false, l == kDgrad || l == kDgradGelu, true)) return {any_tile(M, N), 1};
+  const SplitPlan sp = glu_split_plan(M, N, K, ws_bytes, l);
+  if (sp.splits > 1) return {sp.tile, sp.splits};
+  return {choose_tile(M, N, K, l), 1};
+}
+
 inline size_t ws_round256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 
 // Workspace of a split forward or input-gradient product: the fp32 partials

@@ -114,6 +114,20 @@ def test_glu_workspace_sizes():
     assert _st("enc_glu_workspace_bytes", 8, 8, 8, None) == INV
 
 
+def test_glu_plan_refusals():
+    n = ctypes.c_int()
+    out = ctypes.byref(n)
+    base = [0, 16, 64, 64, 0, out, out, out]
+    _bad("enc_glu_plan", base, [(0, 3, INV), (0, -1, INV), (1, 0, INV), (2, 60, UNS), (3, 12, UNS), (3, 2 ** 30 + 8, UNS),
+                                (5, None, INV), (6, None, INV), (7, None, INV)])
+    for product in (0, 1, 2):
+        for M, H, F in ((1, 8, 8), (2048, 6144, 16384), (70, 6152, 2056), (262000, 8192, 2048)):
+            for ws in (0, 1, 4 * M * 2 * F, 2 ** 62):
+                assert _st("enc_glu_plan", product, M, H, F, ws, out, out, out) == B.ENC_OK and n.value >= 1
+    with pytest.raises(B.EncError):
+        B.glu_plan(7, 16, 64, 64)
+
+
 @no_gpu_only
 def test_attention_refusals():
     need = B.packed_plan_bytes(64, 3)
