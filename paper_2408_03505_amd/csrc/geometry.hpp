@@ -245,10 +245,11 @@ inline float split_sum_us(int M, int N, int s) {
   return static_cast<float>(s + 1) * static_cast<float>(M) * static_cast<float>(N) * (4.f / 4.5e6f);
 }
 
-inline SplitPlan best_split(int M, int N, int K, GemmLayout l) {
+// At most `most` splits; fill: tiles below 128x128 only where they fill the CUs.
+inline SplitPlan best_split(int M, int N, int K, GemmLayout l, int most = kMaxSplits, bool fill = true) {
   SplitPlan best{1, K, {0, 0}};
   float best_us = 0.f;
-  const int max_s = std::min(K / kMinSplitTokens, kMaxSplits);
+  const int max_s = std::min(K / kMinSplitTokens, most);
   const int max_chunk = l == kWgrad ? wgrad_max_chunk(M, N, K) : K;
   const GemmLayout row = l == kWgrad ? kWgradSplit : kSplit;
   for (const TileCost &t : kTiles) {
@@ -256,7 +257,7 @@ inline SplitPlan best_split(int M, int N, int K, GemmLayout l) {
     const bool small = t.bm * t.bn < 128 * 128;
     const long n = tile_count(t, M, N);
     for (int s = 2; s <= max_s && (s == 2 || n * s <= 1024); ++s) {
-      if (small && n * s <= 256) continue;
+      if (small && fill && n * s <= 256) continue;
       const int kc = ((K + s - 1) / s + 63) / 64 * 64;
       if ((K + kc - 1) / kc != s || kc > max_chunk) continue;
       const float us = gemm_cost(t, row, n * s, kc / 64) + split_sum_us(M, N, s);
@@ -292,23 +293,28 @@ inline SplitPlan gemm_split_plan(int M, int N, int K) {
 }
 
 // The gated feed-forward block's products split where the contraction is no multiple
-// of 64, too (the last split's last k-step ends where it does), into no more parts
-// than the workspace holds, and only where the cost model has the split and its
-// second launch (4 us) ahead of the product in one: l is that one's row.
+// of 64, too (the last split's last k-step ends where it does), and only where the cost
+// model has the split and its second launch (4 us) ahead of the product in one: l is
+// that one's row.  Where the workspace holds fewer parts, tile and parts are chosen
+// anew among those that it holds, on small tiles that do not fill the CUs too: the tile
+// of many parts is too large for a few (33 rows, N = 1280, K = 6832: in two parts of
+// 128x128 33.9 us, in two of 64x64 15.0, in one launch 21.6; 150 products with a
+// workspace for some of their parts: a median of 0.86 of the time on the tile of all of
+// them, 1.06 at worst, where up to 1.6 times that in one launch came before).
 inline SplitPlan glu_split_plan(int M, int N, int K, size_t ws_bytes, GemmLayout l) {
-  SplitPlan sp = gemm_split_plan(M, N, (K + 63) / 64 * 64);
-  if (sp.splits == 1) return sp;
-  for (const TileCost &t : kTiles)
-    if (t.bm == sp.tile.bm && t.bn == sp.tile.bn &&
-        gemm_cost(t, kSplit, tile_count(t, M, N) * sp.splits, sp.k_chunk / 64) + split_sum_us(M, N, sp.splits) + 4.f >=
-            pick_tile(M, N, K, l).us)
-      return {1, K, sp.tile};
+  const int whole = (K + 63) / 64 * 64;  // (K and this have as many splits)
+  auto pays = [&](const SplitPlan &sp) {
+    for (const TileCost &t : kTiles)
+      if (sp.splits > 1 && t.bm == sp.tile.bm && t.bn == sp.tile.bn)
+        return gemm_cost(t, kSplit, tile_count(t, M, N) * sp.splits, sp.k_chunk / 64) +
+                   split_sum_us(M, N, sp.splits) + 4.f < pick_tile(M, N, K, l).us;
+    return false;
+  };
+  SplitPlan sp = gemm_split_plan(M, N, whole);
   const size_t room = ws_bytes / (static_cast<size_t>(M) * N * sizeof(float));
-  if (room < static_cast<size_t>(sp.splits)) {
-    const int parts = std::max(static_cast<int>(room), 1);
-    sp.k_chunk = ((K + parts - 1) / parts + 63) / 64 * 64;
-    sp.splits = (K + sp.k_chunk - 1) / sp.k_chunk;
-  }
+  if (pays(sp) && room < static_cast<size_t>(sp.splits))
+    sp = best_split(M, N, whole, kFwd, static_cast<int>(room), false);
+  if (!pays(sp)) return {1, K, sp.tile};
   return sp;
 }
 

@@ -68,6 +68,19 @@ def test_a_smaller_workspace_means_fewer_parts(product, M, H, F):
     assert len({p for p in parts if 1 < p < full}) >= 2  # fewer, and still split
 
 
+@pytest.mark.parametrize("product,M,H,F,rooms", [
+    (B.GLU_UP_BWD_DATA, 33, 1280, 3416, (2, 3)), (B.GLU_UP_BWD_DATA, 64, 1304, 3416, (2, 3)),
+    (B.GLU_UP_FWD, 40, 4104, 1000, (2, 3, 4)), (B.GLU_DOWN_BWD_DATA, 40, 4104, 1000, (2, 3))])
+def test_a_split_cut_to_the_workspace_is_weighed_again(product, M, H, F, rooms):
+    """In a few parts these took longer on the tile of their many parts (128x128) than
+    the product in one launch (16 to 34 us, not 15 to 22)."""
+    N, _ = _dims(product, M, H, F)
+    assert B.glu_plan(product, M, H, F)[:2] == (128, 128)
+    for room in rooms:
+        bm, bn, parts = B.glu_plan(product, M, H, F, 4 * M * N * room)
+        assert parts == 1 or (bm, bn) == (64, 64), (room, bm, bn, parts)
+
+
 # ------------------------------------------------------------------ the products
 
 @gpu
