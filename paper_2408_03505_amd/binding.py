@@ -5,8 +5,8 @@ shapes and contiguity, passes raw device pointers and the current HIP stream
 to the C entry point of the same name, and raises EncError on a non-zero
 status.  All computation runs in the library's HIP kernels; there is no
 fallback path, and a missing library raises at first use.  torch supplies
-device memory and streams (outputs are allocated with torch.empty when the
-caller does not pass them).
+device memory and streams (outputs and workspaces that the caller does not
+pass are allocated with torch.empty, from the memory of the call's stream).
 """
 
 import ctypes
@@ -201,7 +201,7 @@ def _empty(new, shape, dtype, stream, **where):
     """A fresh tensor for a call on `stream`, from that stream's memory: memory of the
     current one may still be in use there, or be given to its next call before
     `stream` is done with it."""
-    if stream is None:
+    if stream is None or stream.cuda_stream == torch._C._cuda_getCurrentRawStream(stream.device_index):
         return new(shape, dtype=dtype, **where)
     with torch.cuda.stream(stream):
         return new(shape, dtype=dtype, **where)
@@ -288,12 +288,12 @@ def encoder_layer_fwd(cfg, params, x, out=None, saved=None, ws=None, stream=None
     device buffer laid out as enc_saved_layout describes."""
     M, H = cfg["batch"] * cfg["seq"], cfg["hidden"]
     _check(x, "x", (M, H))
-    out = _out(out, "out", (M, H), x)
+    out = _out(out, "out", (M, H), x, stream=stream)
     total = saved_layout(cfg)["total"]
-    saved = _out(saved, "saved", (total,), x, torch.uint8)
+    saved = _out(saved, "saved", (total,), x, torch.uint8, stream=stream)
     c, p = make_cfg(cfg), _params_struct(cfg, params)
     if ws is None:  # the layer workspace (split-product partials in the forward)
-        ws = torch.empty(layer_workspace_bytes(cfg), dtype=torch.uint8, device=x.device)
+        ws = _empty(torch.empty, layer_workspace_bytes(cfg), torch.uint8, stream, device=x.device)
     _call("encoder_layer_fwd", ctypes.byref(c), ctypes.byref(p), _ptr(x), _ptr(out), _ptr(saved),
           _ptr(ws), ws.numel() * ws.element_size(), _stream(stream))
     return out, saved
@@ -304,16 +304,16 @@ def encoder_layer_bwd(cfg, params, x, saved, dout, grads=None, dx=None, accumula
     M, H = cfg["batch"] * cfg["seq"], cfg["hidden"]
     _check(x, "x", (M, H))
     _check(dout, "dout", (M, H))
-    dx = _out(dx, "dx", (M, H), x)
+    dx = _out(dx, "dx", (M, H), x, stream=stream)
     shapes = param_shapes(cfg)
     if grads is None:
         if accumulate:
             raise ValueError("accumulate=True needs existing grads")
-        grads = {n: torch.empty(shapes[n], dtype=torch.float32, device=x.device) for n in PARAM_ORDER}
+        grads = {n: _empty(torch.empty, shapes[n], torch.float32, stream, device=x.device) for n in PARAM_ORDER}
     for n in PARAM_ORDER:
         _check(grads[n], "d" + n, shapes[n], torch.float32)
     if ws is None:
-        ws = torch.empty(layer_workspace_bytes(cfg), dtype=torch.uint8, device=x.device)
+        ws = _empty(torch.empty, layer_workspace_bytes(cfg), torch.uint8, stream, device=x.device)
     total = saved_layout(cfg)["total"]
     _check(saved, "saved", (total,), torch.uint8)
     c, p = make_cfg(cfg), _params_struct(cfg, params)
@@ -330,9 +330,9 @@ def enc_ln_fwd(x, gamma, beta, eps, y=None, mean=None, rstd=None, stream=None):
     _check(x, "x", (rows, cols))
     _check(gamma, "gamma", (cols,))
     _check(beta, "beta", (cols,))
-    y = _out(y, "y", (rows, cols), x)
-    mean = _out(mean, "mean", (rows,), x, torch.float32)
-    rstd = _out(rstd, "rstd", (rows,), x, torch.float32)
+    y = _out(y, "y", (rows, cols), x, stream=stream)
+    mean = _out(mean, "mean", (rows,), x, torch.float32, stream=stream)
+    rstd = _out(rstd, "rstd", (rows,), x, torch.float32, stream=stream)
     _call("enc_ln_fwd", rows, cols, _ptr(x), _ptr(gamma), _ptr(beta), float(eps), _ptr(y), _ptr(mean), _ptr(rstd),
           _stream(stream))
     return y, mean, rstd
@@ -345,10 +345,10 @@ def enc_qkv_fwd(y1, w_qkv, b_qkv, qkv=None, ws=None, split=True, stream=None):
     _check(w_qkv, "w_qkv", (A3, H))
     if b_qkv is not None:
         _check(b_qkv, "b_qkv", (A3,))
-    qkv = _out(qkv, "qkv", (M, A3), y1)
+    qkv = _out(qkv, "qkv", (M, A3), y1, stream=stream)
     if A3 % 3:
         raise ValueError("w_qkv rows must be 3*A")
-    wp, wn = _gemm_ws(M, A3, H, ws, split, y1.device)
+    wp, wn = _gemm_ws(M, A3, H, ws, split, y1.device, stream)
     _call("enc_qkv_fwd", M, H, A3 // 3, _ptr(y1), _ptr(w_qkv), _ptr(b_qkv), _ptr(qkv), wp, wn, _stream(stream))
     return qkv
 
@@ -356,8 +356,8 @@ def enc_qkv_fwd(y1, w_qkv, b_qkv, qkv=None, ws=None, split=True, stream=None):
 def enc_attn_fwd(batch, seq, heads, head_dim, qkv, o=None, lse=None, stream=None):
     A = heads * head_dim
     _check(qkv, "qkv", (batch * seq, 3 * A))
-    o = _out(o, "o", (batch * seq, A), qkv)
-    lse = _out(lse, "lse", (batch, heads, seq), qkv, torch.float32)
+    o = _out(o, "o", (batch * seq, A), qkv, stream=stream)
+    lse = _out(lse, "lse", (batch, heads, seq), qkv, torch.float32, stream=stream)
     _call("enc_attn_fwd", batch, seq, heads, head_dim, _ptr(qkv), _ptr(o), _ptr(lse), _stream(stream))
     return o, lse
 
@@ -369,8 +369,8 @@ def enc_oproj_fwd(o, w_o, b_o, resid, h=None, ws=None, split=True, stream=None):
     _check(w_o, "w_o", (H, A))
     _check(b_o, "b_o", (H,))
     _check(resid, "resid", (M, H))
-    h = _out(h, "h", (M, H), o)
-    wp, wn = _gemm_ws(M, H, A, ws, split, o.device)
+    h = _out(h, "h", (M, H), o, stream=stream)
+    wp, wn = _gemm_ws(M, H, A, ws, split, o.device, stream)
     _call("enc_oproj_fwd", M, A, H, _ptr(o), _ptr(w_o), _ptr(b_o), _ptr(resid), _ptr(h), wp, wn, _stream(stream))
     return h
 
@@ -381,9 +381,9 @@ def enc_mlp_up_fwd(y2, w_1, b_1, u=None, g=None, ws=None, split=True, stream=Non
     _check(y2, "y2", (M, H))
     _check(w_1, "w_1", (F, H))
     _check(b_1, "b_1", (F,))
-    u = _out(u, "u", (M, F), y2)
-    g = _out(g, "g", (M, F), y2)
-    wp, wn = _gemm_ws(M, F, H, ws, split, y2.device)
+    u = _out(u, "u", (M, F), y2, stream=stream)
+    g = _out(g, "g", (M, F), y2, stream=stream)
+    wp, wn = _gemm_ws(M, F, H, ws, split, y2.device, stream)
     _call("enc_mlp_up_fwd", M, H, F, _ptr(y2), _ptr(w_1), _ptr(b_1), _ptr(u), _ptr(g), wp, wn, _stream(stream))
     return u, g
 
@@ -395,8 +395,8 @@ def enc_mlp_down_fwd(g, w_2, b_2, resid, out=None, ws=None, split=True, stream=N
     _check(w_2, "w_2", (H, F))
     _check(b_2, "b_2", (H,))
     _check(resid, "resid", (M, H))
-    out = _out(out, "out", (M, H), g)
-    wp, wn = _gemm_ws(M, H, F, ws, split, g.device)
+    out = _out(out, "out", (M, H), g, stream=stream)
+    wp, wn = _gemm_ws(M, H, F, ws, split, g.device, stream)
     _call("enc_mlp_down_fwd", M, F, H, _ptr(g), _ptr(w_2), _ptr(b_2), _ptr(resid), _ptr(out), wp, wn,
           _stream(stream))
     return out
@@ -410,8 +410,8 @@ def enc_mlp_down_bwd_data(dout, w_2, u, du=None, ws=None, split=True, stream=Non
     _check(dout, "dout", (M, H))
     _check(w_2, "w_2", (H, F))
     _check(u, "u", (M, F))
-    du = _out(du, "du", (M, F), dout)
-    wp, wn = _gemm_ws(M, F, H, ws, split, dout.device)
+    du = _out(du, "du", (M, F), dout, stream=stream)
+    wp, wn = _gemm_ws(M, F, H, ws, split, dout.device, stream)
     _call("enc_mlp_down_bwd_data", M, F, H, _ptr(dout), _ptr(w_2), _ptr(u), _ptr(du), wp, wn, _stream(stream))
     return du
 
@@ -421,8 +421,8 @@ def enc_mlp_up_bwd_data(du, w_1, dy2=None, ws=None, split=True, stream=None):
     H = w_1.shape[1]
     _check(du, "du", (M, F))
     _check(w_1, "w_1", (F, H))
-    dy2 = _out(dy2, "dy2", (M, H), du)
-    wp, wn = _gemm_ws(M, H, F, ws, split, du.device)
+    dy2 = _out(dy2, "dy2", (M, H), du, stream=stream)
+    wp, wn = _gemm_ws(M, H, F, ws, split, du.device, stream)
     _call("enc_mlp_up_bwd_data", M, H, F, _ptr(du), _ptr(w_1), _ptr(dy2), wp, wn, _stream(stream))
     return dy2
 
@@ -432,8 +432,8 @@ def enc_oproj_bwd_data(dh, w_o, do=None, ws=None, split=True, stream=None):
     A = w_o.shape[1]
     _check(dh, "dh", (M, H))
     _check(w_o, "w_o", (H, A))
-    do = _out(do, "do", (M, A), dh)
-    wp, wn = _gemm_ws(M, A, H, ws, split, dh.device)
+    do = _out(do, "do", (M, A), dh, stream=stream)
+    wp, wn = _gemm_ws(M, A, H, ws, split, dh.device, stream)
     _call("enc_oproj_bwd_data", M, A, H, _ptr(dh), _ptr(w_o), _ptr(do), wp, wn, _stream(stream))
     return do
 
@@ -443,8 +443,8 @@ def enc_qkv_bwd_data(dqkv, w_qkv, dy1=None, ws=None, split=True, stream=None):
     H = w_qkv.shape[1]
     _check(dqkv, "dqkv", (M, A3))
     _check(w_qkv, "w_qkv", (A3, H))
-    dy1 = _out(dy1, "dy1", (M, H), dqkv)
-    wp, wn = _gemm_ws(M, H, A3, ws, split, dqkv.device)
+    dy1 = _out(dy1, "dy1", (M, H), dqkv, stream=stream)
+    wp, wn = _gemm_ws(M, H, A3, ws, split, dqkv.device, stream)
     _call("enc_qkv_bwd_data", M, H, A3 // 3, _ptr(dqkv), _ptr(w_qkv), _ptr(dy1), wp, wn, _stream(stream))
     return dy1
 
@@ -510,10 +510,10 @@ def enc_linear_bwd_weight(dY, X, dW=None, db=None, accumulate=False, with_db=Tru
     _check(X, "X", (M, K))
     if accumulate and (dW is None or (with_db and db is None)):
         raise ValueError("accumulate=True needs existing dW/db")
-    dW = _out(dW, "dW", (N, K), dY, torch.float32)
+    dW = _out(dW, "dW", (N, K), dY, torch.float32, stream=stream)
     if with_db:
-        db = _out(db, "db", (N,), dY, torch.float32)
-    wp, wn = _wgrad_ws(M, N, K, ws, split, dY.device)
+        db = _out(db, "db", (N,), dY, torch.float32, stream=stream)
+    wp, wn = _wgrad_ws(M, N, K, ws, split, dY.device, stream)
     _call("enc_linear_bwd_weight", M, N, K, _ptr(dY), _ptr(X), _ptr(dW), _ptr(db), 1 if accumulate else 0, wp, wn,
           _stream(stream))
     return dW, db
@@ -570,12 +570,12 @@ def enc_ln_bwd(dy, x, mean, rstd, gamma, dresid=None, dx=None, dgamma=None, dbet
         _check(dresid, "dresid", (rows, cols))
     if accumulate and (dgamma is None or dbeta is None):
         raise ValueError("accumulate=True needs existing dgamma/dbeta")
-    dx = _out(dx, "dx", (rows, cols), x)
-    dgamma = _out(dgamma, "dgamma", (cols,), x, torch.float32)
-    dbeta = _out(dbeta, "dbeta", (cols,), x, torch.float32)
+    dx = _out(dx, "dx", (rows, cols), x, stream=stream)
+    dgamma = _out(dgamma, "dgamma", (cols,), x, torch.float32, stream=stream)
+    dbeta = _out(dbeta, "dbeta", (cols,), x, torch.float32, stream=stream)
     need = ln_bwd_workspace_bytes(rows, cols)
     if ws is None:
-        ws = torch.empty(need, dtype=torch.uint8, device=x.device)
+        ws = _empty(torch.empty, need, torch.uint8, stream, device=x.device)
     _call("enc_ln_bwd", rows, cols, _ptr(dy), _ptr(x), _ptr(mean), _ptr(rstd), _ptr(gamma), _ptr(dresid), _ptr(dx),
           _ptr(dgamma), _ptr(dbeta), 1 if accumulate else 0, _ptr(ws), ws.numel() * ws.element_size(),
           _stream(stream))
@@ -589,10 +589,10 @@ def enc_attn_bwd(batch, seq, heads, head_dim, qkv, o, lse, do, dqkv=None, ws=Non
     _check(o, "o", (M, A))
     _check(lse, "lse", (batch, heads, seq), torch.float32)
     _check(do, "do", (M, A))
-    dqkv = _out(dqkv, "dqkv", (M, 3 * A), qkv)
+    dqkv = _out(dqkv, "dqkv", (M, 3 * A), qkv, stream=stream)
     need = attn_bwd_workspace_bytes(batch, seq, heads, head_dim)
     if ws is None:
-        ws = torch.empty(need, dtype=torch.uint8, device=qkv.device)
+        ws = _empty(torch.empty, need, torch.uint8, stream, device=qkv.device)
     _call("enc_attn_bwd", batch, seq, heads, head_dim, _ptr(qkv), _ptr(o), _ptr(lse), _ptr(do), _ptr(dqkv),
           _ptr(ws), ws.numel() * ws.element_size(), _stream(stream))
     return dqkv
@@ -619,7 +619,7 @@ def enc_attn_bwd_noalloc(batch, seq, heads, head_dim, qkv, o, lse, do, dqkv, str
 def enc_calib_mfma(blocks, iters, out=None, stream=None, device="cuda"):
     """MFMA-only reference loop: blocks * 4 * iters * 32 * 16384 flops."""
     if out is None:
-        out = torch.empty(blocks * 256, dtype=torch.float32, device=device)
+        out = _empty(torch.empty, blocks * 256, torch.float32, stream, device=device)
     _check(out, "out", (blocks * 256,), torch.float32)
     _call("enc_calib_mfma", blocks, iters, _ptr(out), _stream(stream))
     return out
@@ -718,9 +718,9 @@ def encoder_parallel_fwd(cfg, params, x, out=None, saved=None, stream=None):
     """Forward of the parallel block. Returns (out, saved)."""
     M, H = cfg["batch"] * cfg["seq"], cfg["hidden"]
     _check(x, "x", (M, H))
-    out = _out(out, "out", (M, H), x)
+    out = _out(out, "out", (M, H), x, stream=stream)
     total = parallel_saved_layout(cfg)["total"]
-    saved = _out(saved, "saved", (total,), x, torch.uint8)
+    saved = _out(saved, "saved", (total,), x, torch.uint8, stream=stream)
     c, p = make_cfg(cfg), _pparams_struct(cfg, params)
     _call("encoder_parallel_fwd", ctypes.byref(c), ctypes.byref(p), _ptr(x), _ptr(out), _ptr(saved), _stream(stream))
     return out, saved
@@ -731,16 +731,16 @@ def encoder_parallel_bwd(cfg, params, x, saved, dout, grads=None, dx=None, accum
     M, H = cfg["batch"] * cfg["seq"], cfg["hidden"]
     _check(x, "x", (M, H))
     _check(dout, "dout", (M, H))
-    dx = _out(dx, "dx", (M, H), x)
+    dx = _out(dx, "dx", (M, H), x, stream=stream)
     shapes = parallel_param_shapes(cfg)
     if grads is None:
         if accumulate:
             raise ValueError("accumulate=True needs existing grads")
-        grads = {n: torch.empty(shapes[n], dtype=torch.float32, device=x.device) for n in PPARAM_ORDER}
+        grads = {n: _empty(torch.empty, shapes[n], torch.float32, stream, device=x.device) for n in PPARAM_ORDER}
     for n in PPARAM_ORDER:
         _check(grads[n], "d" + n, shapes[n], torch.float32)
     if ws is None:
-        ws = torch.empty(parallel_workspace_bytes(cfg), dtype=torch.uint8, device=x.device)
+        ws = _empty(torch.empty, parallel_workspace_bytes(cfg), torch.uint8, stream, device=x.device)
     _check(saved, "saved", (parallel_saved_layout(cfg)["total"],), torch.uint8)
     c, p = make_cfg(cfg), _pparams_struct(cfg, params)
     g = EncPGrads(*[_ptr(grads[n]) for n in PPARAM_ORDER])
@@ -761,8 +761,8 @@ def enc_qk_norm_fwd(heads, head_dim, qkv, qn_g, qn_b, kn_g, kn_b, eps, qkvn=None
     _check(qkv, "qkv", (M, 3 * A))
     for n, t in (("qn_g", qn_g), ("qn_b", qn_b), ("kn_g", kn_g), ("kn_b", kn_b)):
         _check(t, n, (head_dim,))
-    qkvn = _out(qkvn, "qkvn", (M, 3 * A), qkv)
-    stats = _out(stats, "stats", (M, heads, 4), qkv, torch.float32)
+    qkvn = _out(qkvn, "qkvn", (M, 3 * A), qkv, stream=stream)
+    stats = _out(stats, "stats", (M, heads, 4), qkv, torch.float32, stream=stream)
     _call("enc_qk_norm_fwd", M, heads, head_dim, _ptr(qkv), _ptr(qn_g), _ptr(qn_b), _ptr(kn_g), _ptr(kn_b),
           float(eps), _ptr(qkvn), _ptr(stats), _stream(stream))
     return qkvn, stats
@@ -778,16 +778,17 @@ def enc_qk_norm_bwd(heads, head_dim, dqkvn, qkv, stats, qn_g, kn_g, dqkv=None, g
     _check(stats, "stats", (M, heads, 4), torch.float32)
     _check(qn_g, "qn_g", (head_dim,))
     _check(kn_g, "kn_g", (head_dim,))
-    dqkv = _out(dqkv, "dqkv", (M, 3 * A), qkv)
+    dqkv = _out(dqkv, "dqkv", (M, 3 * A), qkv, stream=stream)
     names = ("qn_g", "qn_b", "kn_g", "kn_b")
     if grads is None:
         if accumulate:
             raise ValueError("accumulate=True needs existing grads")
-        grads = {n: torch.empty(head_dim, dtype=torch.float32, device=qkv.device) for n in names}
+        grads = {n: _empty(torch.empty, head_dim, torch.float32, stream, device=qkv.device) for n in names}
     for n in names:
         _check(grads[n], "d" + n, (head_dim,), torch.float32)
     if ws is None:
-        ws = torch.empty(qk_norm_bwd_workspace_bytes(M, heads, head_dim), dtype=torch.uint8, device=qkv.device)
+        need = qk_norm_bwd_workspace_bytes(M, heads, head_dim)
+        ws = _empty(torch.empty, need, torch.uint8, stream, device=qkv.device)
     _call("enc_qk_norm_bwd", M, heads, head_dim, _ptr(dqkvn), _ptr(qkv), _ptr(stats), _ptr(qn_g), _ptr(kn_g),
           _ptr(dqkv), *[_ptr(grads[n]) for n in names], 1 if accumulate else 0, _ptr(ws), ws.numel(),
           _stream(stream))
@@ -800,8 +801,8 @@ def enc_qkv_bwd_data_add(dqkv, w_qkv, addend, dy=None, ws=None, split=True, stre
     _check(dqkv, "dqkv", (M, A3))
     _check(w_qkv, "w_qkv", (A3, H))
     _check(addend, "addend", (M, H))
-    dy = _out(dy, "dy", (M, H), dqkv)
-    wp, wn = _gemm_ws(M, H, A3, ws, split, dqkv.device)
+    dy = _out(dy, "dy", (M, H), dqkv, stream=stream)
+    wp, wn = _gemm_ws(M, H, A3, ws, split, dqkv.device, stream)
     _call("enc_qkv_bwd_data_add", M, H, A3 // 3, _ptr(dqkv), _ptr(w_qkv), _ptr(addend), _ptr(dy), wp, wn,
           _stream(stream))
     return dy
@@ -1022,11 +1023,11 @@ def enc_patch_embed_fwd(images, patch, w_pe, b_pe, pos, cls=None, patches=None, 
     _check(pos, "pos", (S, hidden))
     if has_cls:
         _check(cls, "cls", (hidden,))
-    patches = _out(patches, "patches", (B * N, kp), images)
-    x0 = _out(x0, "x0", (B * S, hidden), images)
+    patches = _out(patches, "patches", (B * N, kp), images, stream=stream)
+    x0 = _out(x0, "x0", (B * S, hidden), images, stream=stream)
     need = patch_embed_workspace_bytes(B, C, ih, iw, patch, hidden, has_cls)
     if ws is None and need:
-        ws = torch.empty(need, dtype=torch.uint8, device=images.device)
+        ws = _empty(torch.empty, need, torch.uint8, stream, device=images.device)
     _call("enc_patch_embed_fwd", B, C, ih, iw, patch, hidden, int(has_cls), _ptr(images), _ptr(w_pe), _ptr(b_pe),
           _ptr(cls), _ptr(pos), _ptr(patches), _ptr(x0), _ptr(ws), ws.numel() if ws is not None else 0,
           _stream(stream))
@@ -1049,12 +1050,12 @@ def enc_patch_embed_bwd(images_shape, patch, dx0, patches, has_cls, grads=None, 
     if grads is None:
         if accumulate:
             raise ValueError("accumulate=True needs existing grads")
-        grads = {k: torch.empty(v, dtype=torch.float32, device=dx0.device) for k, v in shapes.items()}
+        grads = {k: _empty(torch.empty, v, torch.float32, stream, device=dx0.device) for k, v in shapes.items()}
     for k, v in shapes.items():
         _check(grads[k], "d" + k, v, torch.float32)
     need = patch_embed_workspace_bytes(B, C, ih, iw, patch, hidden, has_cls)
     if ws is None and need:
-        ws = torch.empty(need, dtype=torch.uint8, device=dx0.device)
+        ws = _empty(torch.empty, need, torch.uint8, stream, device=dx0.device)
     _call("enc_patch_embed_bwd", B, C, ih, iw, patch, hidden, int(bool(has_cls)), _ptr(dx0), _ptr(patches),
           _ptr(grads["w_pe"]), _ptr(grads["b_pe"]), _ptr(grads.get("cls")), _ptr(grads["pos"]),
           1 if accumulate else 0, _ptr(ws), ws.numel() if ws is not None else 0, _stream(stream))
@@ -1082,8 +1083,8 @@ def encoder_stack_fwd(cfg, layer_params, lnf_g, lnf_b, x0, out=None, saved=None,
     _check(x0, "x0", (M, H))
     _check(lnf_g, "lnf_g", (H,))
     _check(lnf_b, "lnf_b", (H,))
-    out = _out(out, "out", (M, H), x0)
-    saved = _out(saved, "saved", (stack_saved_bytes(cfg, L),), x0, torch.uint8)
+    out = _out(out, "out", (M, H), x0, stream=stream)
+    saved = _out(saved, "saved", (stack_saved_bytes(cfg, L),), x0, torch.uint8, stream=stream)
     arr = (EncParams * L)(*[_params_struct(cfg, p) for p in layer_params])
     c = make_cfg(cfg)
     _call("encoder_stack_fwd", ctypes.byref(c), L, ctypes.cast(arr, _p), _ptr(lnf_g), _ptr(lnf_b), _ptr(x0),
@@ -1099,21 +1100,21 @@ def encoder_stack_bwd(cfg, layer_params, lnf_g, x0, saved, dout, grads=None, lnf
     _check(x0, "x0", (M, H))
     _check(dout, "dout", (M, H))
     _check(saved, "saved", (stack_saved_bytes(cfg, L),), torch.uint8)
-    dx0 = _out(dx0, "dx0", (M, H), x0)
+    dx0 = _out(dx0, "dx0", (M, H), x0, stream=stream)
     shapes = param_shapes(cfg)
     if grads is None:
         if accumulate:
             raise ValueError("accumulate=True needs existing grads")
-        grads = [{n: torch.empty(shapes[n], dtype=torch.float32, device=x0.device) for n in PARAM_ORDER}
+        grads = [{n: _empty(torch.empty, shapes[n], torch.float32, stream, device=x0.device) for n in PARAM_ORDER}
                  for _ in range(L)]
-        lnf_grads = tuple(torch.empty(H, dtype=torch.float32, device=x0.device) for _ in range(2))
+        lnf_grads = tuple(_empty(torch.empty, H, torch.float32, stream, device=x0.device) for _ in range(2))
     for g in grads:
         for n in PARAM_ORDER:
             _check(g[n], "d" + n, shapes[n], torch.float32)
     for t in lnf_grads:
         _check(t, "dlnf", (H,), torch.float32)
     if ws is None:
-        ws = torch.empty(stack_workspace_bytes(cfg, L), dtype=torch.uint8, device=x0.device)
+        ws = _empty(torch.empty, stack_workspace_bytes(cfg, L), torch.uint8, stream, device=x0.device)
     arr = (EncParams * L)(*[_params_struct(cfg, p) for p in layer_params])
     garr = (EncGrads * L)(*[EncGrads(*[_ptr(g[n]) for n in PARAM_ORDER]) for g in grads])
     c = make_cfg(cfg)
