@@ -15,9 +15,12 @@ constexpr float kLazyRescale = 8.0f;  // forward: rescale when a query's maximum
 constexpr int kPrefetchMaxD = 80;     // head dims whose registers hold a tile's operands read ahead
 
 // 2^x on the hardware exponential (v_exp_f32).  Every argument here is a
-// logit minus a running maximum or the log-sum-exp, so x <= 0 up to rounding
-// and -inf for masked keys: results lie in [0, 1] and those below the fp32
-// normal range flush to zero, which only drops weights under 2^-126.
+// logit minus a running maximum or the log-sum-exp.  Of a key that the query
+// sees it is at most kLazyRescale (the maximum moves lazily) or, of the
+// log-sum-exp, 0 up to rounding; results below the fp32 normal range flush to
+// zero, which only drops weights under 2^-126.  Of a masked key it is -inf, or,
+// in a causal backward, which masks the results, anything: later keys are not
+// in the log-sum-exp, and the result may be +inf.
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 
 template <int D>

@@ -201,6 +201,29 @@ def test_attention_of_large_logits(d):
     within(dqkv, ref, bound)
 
 
+@pytest.mark.parametrize("heads,kv,d", [(2, 2, 64), (4, 1, 80), (3, 1, 128)])
+def test_causal_attention_whose_unseen_logits_overflow(heads, kv, d):
+    """Keys that grow within each tile of 32: those that a query does not see exceed its
+    log-sum-exp by so much that their weights, formed before the mask, are infinite."""
+    T, cu = 300, [0, 300]
+    announce(f"packed causal attention heads={heads}/{kv} d={d} large unseen logits")
+    qkv, do, _ = _attn_inputs(cu, T, heads, kv, d, 25, scale=10.0)
+    x = qkv.view(T, heads + 2 * kv, d)
+    x[:, heads:heads + kv] *= ((torch.arange(T) % 32 + 1) / 32).to(BF)[:, None, None]
+    plan = _plan(cu, T)
+    o, lse = B.enc_attn_packed_fwd(1, heads, kv, d, cuda(qkv), plan, True)
+    dqkv = B.enc_attn_packed_bwd(1, heads, kv, d, cuda(qkv), o, lse, cuda(do), plan, True)
+    ref, rlse, bound, lbound = P.packed_attention_fwd(f64(qkv), cu, heads, kv, d, True)
+    v = f64(x)
+    for h in range(heads):
+        over = v[:32, h] @ v[:32, heads + h // (heads // kv)].T / np.sqrt(d) - rlse[h, :32, None]
+        assert (np.triu(over, 1) > 129 * np.log(2)).any()
+    within(o, ref, bound)
+    within(lse, rlse, lbound)
+    ref, bound = P.packed_attention_bwd(f64(qkv), cu, heads, kv, d, True, f64(do))
+    within(dqkv, ref, bound)
+
+
 @pytest.mark.parametrize("low", [torch.finfo(BF).min, float("-inf")])
 @pytest.mark.parametrize("causal", [False, True])
 @pytest.mark.parametrize("heads,kv,d", [(2, 2, 64), (4, 1, 80), (2, 1, 128)])
