@@ -110,8 +110,7 @@ __device__ __forceinline__ bool query_work(const PackedAttnArgs &p, int wid, Que
 }
 
 // Per-lane byte offsets of this wave's loads of a tile (rows ld elements
-// apart); lanes past the head's width get one past every extent, which loads
-// zero without touching memory.
+// apart); lanes past the head's width ask for nothing (a sequence may span 4 GiB).
 template <int D, int KT, int NW, int N>
 __device__ __forceinline__ void packed_voff(uint32_t (&v)[N], int wid, int lane, int ld, bool perm) {
   static_assert(N == TileLoads<KT, NW>::N, "one offset per load");
@@ -119,7 +118,7 @@ __device__ __forceinline__ void packed_voff(uint32_t (&v)[N], int wid, int lane,
   for (int i = 0; i < N; ++i) {
     const int o = (wid * N + i) * 1024 + lane * 16;
     const int pr = o >> 8, c = ((o & 255) >> 4) ^ tsw(pr);
-    v[i] = c * 8 < D ? static_cast<uint32_t>(((perm ? perm23(pr) : pr) * ld + c * 8) * 2) : 0x80000000u;
+    v[i] = c * 8 < D ? static_cast<uint32_t>(((perm ? perm23(pr) : pr) * ld + c * 8) * 2) : kPastEnd;
   }
 }
 

@@ -739,9 +739,6 @@ bool launch_any(const GemmArgs &a, hipStream_t s) {
 // 537 -> 520, 410 -> 397.
 // ---------------------------------------------------------------------------
 
-// A buffer offset past the end of every operand: such a load returns zero.
-constexpr uint32_t kPastEnd = 0xfffffff0u;
-
 // One operand's half tiles: NWV waves of 2 * FH fragments of 16 rows each;
 // half h holds each wave's fragments [h * FH, (h + 1) * FH).
 template <int NWV, int FH, bool TRANS>

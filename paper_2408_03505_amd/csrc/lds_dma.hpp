@@ -18,6 +18,10 @@ __device__ __forceinline__ u32x4_t make_rsrc(const void *base, uint32_t nbytes) 
                  static_cast<uint32_t>(kRsrcWord3)};
 }
 
+// A buffer offset past the end of every operand: such a load returns zero without
+// touching memory.
+constexpr uint32_t kPastEnd = 0xfffffff0u;
+
 // One 16-byte-per-lane buffer load written straight to LDS at
 // lds_addr + 16 * lane.  Issued as inline asm so that the compiler does not
 // wrap every later LDS access and barrier in a full vmcnt(0) wait; the

@@ -424,6 +424,67 @@ def test_attention_at_the_end_of_the_largest_tensor():
     within(dqkv[cu[0]:], ref, bound)
 
 
+def test_attention_of_a_sequence_beyond_2_gib():
+    """One sequence whose rows span more than 2^31 bytes, heads of 80, whose tiles' last
+    columns lie past the head: queries and keys from its first to its last rows, in
+    64 bits from the kernel's own log-sum-exp."""
+    heads, kv, d, T = 96, 24, 80, 100003
+    A, W = heads * d, (heads + 2 * kv) * d
+    assert T * W * 2 > 2 ** 31
+    announce(f"packed attention of one sequence of {T} rows, {T * W * 2} bytes")
+    g = torch.Generator(device="cuda").manual_seed(61)
+    qkv = torch.randn(T, W, generator=g, dtype=BF, device="cuda")
+    do = torch.randn(T, A, generator=g, dtype=BF, device="cuda")
+    plan = _plan([0, T], T)
+    o, lse = B.enc_attn_packed_fwd(1, heads, kv, d, qkv, plan)
+    dqkv = B.enc_attn_packed_bwd(1, heads, kv, d, qkv, o, lse, do, plan)
+    rows = torch.tensor([0, 1, 46603, 93206, 93207, 99999, T - 1], device="cuda")
+    n, F = T, P.FP32
+    for h in (0, heads - 1):
+        j = h // (heads // kv)
+        col = lambda t, i: t[:, i * d:(i + 1) * d].double()  # noqa: E731
+        q, k, v, dh, oh = col(qkv, h), col(qkv, heads + j), col(qkv, heads + kv + j), col(do, h), col(o, h)
+        s = q[rows] @ k.t() / d ** 0.5
+        size = (q[rows].abs() @ k.abs().t() / d ** 0.5).amax(1, keepdim=True)
+        rlse = torch.logsumexp(s, 1)
+        p = (s - rlse[:, None]).exp()
+        # the oracle's bounds (oracle/packed.py)
+        ds = F * ((d + 4) * size + 4 * s.amax(1, keepdim=True).abs() + 8)
+        ro, lb = p @ v, (2 * ds + (n + 16) * F)[:, 0] + 4 * F * rlse.abs()
+        ob = (P.BF16 + 2 * ds + 2 * (n + 16) * F) * (p @ v.abs()) + P.BF16 * ro.abs() * (1 + P.BF16)
+        within(o[rows, h * d:(h + 1) * d], f64(ro), f64(ob))
+        within(lse[h, rows], f64(rlse), f64(lb))
+        rel = F * ((d + 4) * size + 8 * rlse[:, None].abs() + 8) + lb[:, None]
+        dP, D = dh[rows] @ v.t(), (dh[rows] * ro).sum(1, keepdim=True)
+        e = p * (dP - D)
+        edd = (dh[rows].abs() * (ob + (d + 4) * F * ro.abs())).sum(1, keepdim=True)
+        eds = (P.BF16 + rel) * e.abs() + p * (1 + rel) * ((d + 4) * F * (dh[rows].abs() @ v.abs().t()) + edd)
+        ref, b = e @ k / d ** 0.5, (eds + (n + 16) * F * e.abs()) @ k.abs() / d ** 0.5
+        within(dqkv[rows, h * d:(h + 1) * d], f64(ref), f64(b + P.BF16 * (ref.abs() + b)))
+    # dK and dV of these rows, over the queries of the four heads that share them, from the
+    # kernel's own o and lse
+    for j in (0, kv - 1):
+        dk, dv = torch.zeros(len(rows), d, dtype=torch.float64, device="cuda"), None
+        dv, kb, vb = dk.clone(), dk.clone(), dk.clone()
+        k, v = col(qkv, heads + j)[rows], col(qkv, heads + kv + j)[rows]
+        for h in range(j * heads // kv, (j + 1) * heads // kv):
+            q, dh, oh, L = col(qkv, h), col(do, h), col(o, h), lse[h].double()
+            s = q @ k.t() / d ** 0.5
+            p = (s - L[:, None]).exp()
+            dP, D = dh @ v.t(), (dh * oh).sum(1, keepdim=True)
+            e = p * (dP - D)
+            rel = F * ((d + 4) * (q.abs() @ k.abs().t() / d ** 0.5) + 12 * L.abs()[:, None] + 8)
+            eds = (P.BF16 + rel) * e.abs() + p * (1 + rel) * (d + 4) * F * (
+                dh.abs() @ v.abs().t() + (dh.abs() * oh.abs()).sum(1, keepdim=True))
+            add = (heads // kv * n + 16) * F
+            dk += e.t() @ q / d ** 0.5
+            dv += p.t() @ dh
+            kb += (eds + add * e.abs()).t() @ q.abs() / d ** 0.5
+            vb += ((P.BF16 + rel + add) * p).t() @ dh.abs()
+        for i, ref, b in ((heads + j, dk, kb), (heads + kv + j, dv, vb)):
+            within(dqkv[rows, i * d:(i + 1) * d], f64(ref), f64(b + P.BF16 * (ref.abs() + b)))
+
+
 # ------------------------------------------------------------------ a packed layer
 
 @pytest.mark.parametrize("heads,kv,d,act", [(3, 3, 64, "silu"), (4, 1, 80, "gelu")])
