@@ -226,9 +226,9 @@ def prepare(case, seed):
         from paper_2408_03505_amd import binding as B
         M, H, F = case["rows"], case["hidden"], case["mlp"]
         if case["bwd"]:
-            need = max(B.linear_workspace_bytes(M, F, H), B.linear_workspace_bytes(M, H, 2 * F))
+            need = max(B.glu_workspace_bytes(M, F, H), B.glu_workspace_bytes(M, H, 2 * F))
         else:
-            need = B.linear_workspace_bytes(M, 2 * F, H)
+            need = B.glu_workspace_bytes(M, 2 * F, H)
         st["ws"] = torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
     return st
 
