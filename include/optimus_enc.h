@@ -466,10 +466,20 @@ int enc_qkv_bwd_data_add(int M, int H, int A, const enc_bf16 *dqkv,
  *
  * qkv rows are packed [heads + 2 kv_heads][head_dim]: queries, keys, values.
  * Query head h reads key and value head h / (heads / kv_heads); with
- * kv_heads = heads this is the qkv of the other entry points.  The projection
- * that writes it is enc_qkv_fwd with 3A = (heads + 2 kv_heads) * head_dim.
+ * kv_heads = heads this is the qkv of the other entry points.  Its projection
+ * is that of enc_qkv_fwd, with a width that need not be a multiple of 3: the two
+ * calls below, and enc_linear_bwd_weight(tokens, width, H) for its weight.
  * Limits: heads a multiple of kv_heads and at most 65536, at most 65536
  * sequences, head_dim 64, 80 or 128. */
+
+/* [Packed block step: fused Q, K, V projection, any head layout]
+ * enc_qkv_fwd, enc_qkv_bwd_data and their results for a qkv of `width` =
+ * (heads + 2 kv_heads) * head_dim columns: w_qkv [width, H], b_qkv [width] or
+ * NULL; ws as for (tokens, width, H) and (tokens, H, width). */
+int enc_packed_qkv_fwd(int tokens, int H, int width, const enc_bf16 *y1, const enc_bf16 *w_qkv, const enc_bf16 *b_qkv,
+                       enc_bf16 *qkv, void *ws, size_t ws_bytes, enc_stream_t stream);
+int enc_packed_qkv_bwd_data(int tokens, int H, int width, const enc_bf16 *dqkv, const enc_bf16 *w_qkv, enc_bf16 *dy1,
+                            void *ws, size_t ws_bytes, enc_stream_t stream);
 
 /* [Packed block step: rotary positions in place of learned ones]
  * Rotary positions with three axes (time, height, width).  pos [M, 3] int32

@@ -108,6 +108,8 @@ _SIGS = {
     "enc_qk_norm_bwd_workspace_bytes": [_i, _i, _i, ctypes.POINTER(_sz)],
     "enc_qk_norm_bwd": [_i, _i, _i, _p, _p, _p, _p, _p, _p, _p, _p, _p, _p, _i, _p, _sz, _p],
     "enc_qkv_bwd_data_add": [_i, _i, _i, _p, _p, _p, _p, _p, _sz, _p],
+    "enc_packed_qkv_fwd": [_i, _i, _i, _p, _p, _p, _p, _p, _sz, _p],
+    "enc_packed_qkv_bwd_data": [_i, _i, _i, _p, _p, _p, _p, _sz, _p],
     "enc_rope_fwd": [_i, _i, _i, _i, _i, _i, _i, _i, _p, _p, _p, _p, _p],
     "enc_rope_bwd": [_i, _i, _i, _i, _i, _i, _i, _i, _p, _p, _p, _p, _p],
     "enc_packed_plan_bytes": [_i, _i, ctypes.POINTER(_sz)],
@@ -339,6 +341,7 @@ def enc_ln_fwd(x, gamma, beta, eps, y=None, mean=None, rstd=None, stream=None):
 
 
 def enc_qkv_fwd(y1, w_qkv, b_qkv, qkv=None, ws=None, split=True, stream=None):
+    """w_qkv [3A, H], or of a packed batch's (heads + 2 kv_heads) * head_dim rows."""
     M, H = y1.shape
     A3 = w_qkv.shape[0]
     _check(y1, "y1", (M, H))
@@ -346,10 +349,9 @@ def enc_qkv_fwd(y1, w_qkv, b_qkv, qkv=None, ws=None, split=True, stream=None):
     if b_qkv is not None:
         _check(b_qkv, "b_qkv", (A3,))
     qkv = _out(qkv, "qkv", (M, A3), y1, stream=stream)
-    if A3 % 3:
-        raise ValueError("w_qkv rows must be 3*A")
     wp, wn = _gemm_ws(M, A3, H, ws, split, y1.device, stream)
-    _call("enc_qkv_fwd", M, H, A3 // 3, _ptr(y1), _ptr(w_qkv), _ptr(b_qkv), _ptr(qkv), wp, wn, _stream(stream))
+    name, width = ("enc_packed_qkv_fwd", A3) if A3 % 3 else ("enc_qkv_fwd", A3 // 3)
+    _call(name, M, H, width, _ptr(y1), _ptr(w_qkv), _ptr(b_qkv), _ptr(qkv), wp, wn, _stream(stream))
     return qkv
 
 
@@ -445,7 +447,8 @@ def enc_qkv_bwd_data(dqkv, w_qkv, dy1=None, ws=None, split=True, stream=None):
     _check(w_qkv, "w_qkv", (A3, H))
     dy1 = _out(dy1, "dy1", (M, H), dqkv, stream=stream)
     wp, wn = _gemm_ws(M, H, A3, ws, split, dqkv.device, stream)
-    _call("enc_qkv_bwd_data", M, H, A3 // 3, _ptr(dqkv), _ptr(w_qkv), _ptr(dy1), wp, wn, _stream(stream))
+    name, width = ("enc_packed_qkv_bwd_data", A3) if A3 % 3 else ("enc_qkv_bwd_data", A3 // 3)
+    _call(name, M, H, width, _ptr(dqkv), _ptr(w_qkv), _ptr(dy1), wp, wn, _stream(stream))
     return dy1
 
 
@@ -554,8 +557,8 @@ def enc_qkv_bwd_weight(dqkv, y1, dw_qkv, db_qkv, accumulate=False, ws=None, spli
     H = y1.shape[1]
     _check(dqkv, "dqkv", (M, A3)); _check(y1, "y1", (M, H))
     _check(dw_qkv, "dw_qkv", (A3, H), torch.float32); _check(db_qkv, "db_qkv", (A3,), torch.float32)
-    return _named_wgrad("enc_qkv_bwd_weight", M, H, A3 // 3, A3, H, dqkv, y1, dw_qkv, db_qkv, accumulate, ws, split,
-                        stream)
+    name, a, b = ("enc_linear_bwd_weight", A3, H) if A3 % 3 else ("enc_qkv_bwd_weight", H, A3 // 3)
+    return _named_wgrad(name, M, a, b, A3, H, dqkv, y1, dw_qkv, db_qkv, accumulate, ws, split, stream)
 
 
 def enc_ln_bwd(dy, x, mean, rstd, gamma, dresid=None, dx=None, dgamma=None, dbeta=None, accumulate=False,

@@ -599,19 +599,31 @@ int enc_ln_fwd(int rows, int cols, const enc_bf16 *x, const enc_bf16 *gamma, con
   return launched(fn);
 }
 
-int enc_qkv_fwd(int M, int H, int A, const enc_bf16 *y1, const enc_bf16 *w_qkv, const enc_bf16 *b_qkv, enc_bf16 *qkv,
-                void *ws, size_t ws_bytes, enc_stream_t stream) {
-  const char *fn = "enc_qkv_fwd";
-  int r = linear_dims(fn, M, {H, A, 3 * A});
-  if (r) return r;
+// the projection to W columns, its dimensions checked
+static int qkv_fwd(const char *fn, int M, int H, int W, const enc_bf16 *y1, const enc_bf16 *w_qkv,
+                   const enc_bf16 *b_qkv, enc_bf16 *qkv, void *ws, size_t ws_bytes, enc_stream_t stream) {
   PtrCheck c(fn);
   c.req(y1, "y1").req(w_qkv, "w_qkv").opt(b_qkv, "b_qkv").req(qkv, "qkv");
   if (c.code) return c.code;
-  if ((r = check_gemm_ws(fn, ws, ws_bytes, M, 3 * A, H))) return r;
-  if (!gemm_fwd(M, 3 * A, H, y1, w_qkv, b_qkv, nullptr, qkv, nullptr, b_qkv ? Epi::kBias : Epi::kPlain, ws,
-                ws_bytes, as_stream(stream)))
+  if (int r = check_gemm_ws(fn, ws, ws_bytes, M, W, H)) return r;
+  if (!gemm_fwd(M, W, H, y1, w_qkv, b_qkv, nullptr, qkv, nullptr, b_qkv ? Epi::kBias : Epi::kPlain, ws, ws_bytes,
+                as_stream(stream)))
     return refused_after_checks(fn);
   return launched(fn);
+}
+
+int enc_qkv_fwd(int M, int H, int A, const enc_bf16 *y1, const enc_bf16 *w_qkv, const enc_bf16 *b_qkv, enc_bf16 *qkv,
+                void *ws, size_t ws_bytes, enc_stream_t stream) {
+  const char *fn = "enc_qkv_fwd";
+  if (int r = linear_dims(fn, M, {H, A, 3 * A})) return r;
+  return qkv_fwd(fn, M, H, 3 * A, y1, w_qkv, b_qkv, qkv, ws, ws_bytes, stream);
+}
+
+int enc_packed_qkv_fwd(int tokens, int H, int width, const enc_bf16 *y1, const enc_bf16 *w_qkv, const enc_bf16 *b_qkv,
+                       enc_bf16 *qkv, void *ws, size_t ws_bytes, enc_stream_t stream) {
+  const char *fn = "enc_packed_qkv_fwd";
+  if (int r = linear_dims(fn, tokens, {H, width})) return r;
+  return qkv_fwd(fn, tokens, H, width, y1, w_qkv, b_qkv, qkv, ws, ws_bytes, stream);
 }
 
 int enc_attn_fwd(int batch, int seq, int heads, int head_dim, const enc_bf16 *qkv, enc_bf16 *o, float *lse,
@@ -710,18 +722,29 @@ int enc_oproj_bwd_data(int M, int A, int H, const enc_bf16 *dh, const enc_bf16 *
   return launched(fn);
 }
 
-int enc_qkv_bwd_data(int M, int H, int A, const enc_bf16 *dqkv, const enc_bf16 *w_qkv, enc_bf16 *dy1, void *ws,
-                     size_t ws_bytes, enc_stream_t stream) {
-  const char *fn = "enc_qkv_bwd_data";
-  int r = linear_dims(fn, M, {H, A, 3 * A});
-  if (r) return r;
+// its input gradient, the dimensions checked
+static int qkv_bwd_data(const char *fn, int M, int H, int W, const enc_bf16 *dqkv, const enc_bf16 *w_qkv,
+                        enc_bf16 *dy1, void *ws, size_t ws_bytes, enc_stream_t stream) {
   PtrCheck c(fn);
   c.req(dqkv, "dqkv").req(w_qkv, "w_qkv").req(dy1, "dy1");
   if (c.code) return c.code;
-  if ((r = check_gemm_ws(fn, ws, ws_bytes, M, H, 3 * A))) return r;
-  if (!gemm_dgrad(M, 3 * A, H, dqkv, w_qkv, nullptr, dy1, ws, ws_bytes, as_stream(stream)))
-    return refused_after_checks(fn);
+  if (int r = check_gemm_ws(fn, ws, ws_bytes, M, H, W)) return r;
+  if (!gemm_dgrad(M, W, H, dqkv, w_qkv, nullptr, dy1, ws, ws_bytes, as_stream(stream))) return refused_after_checks(fn);
   return launched(fn);
+}
+
+int enc_qkv_bwd_data(int M, int H, int A, const enc_bf16 *dqkv, const enc_bf16 *w_qkv, enc_bf16 *dy1, void *ws,
+                     size_t ws_bytes, enc_stream_t stream) {
+  const char *fn = "enc_qkv_bwd_data";
+  if (int r = linear_dims(fn, M, {H, A, 3 * A})) return r;
+  return qkv_bwd_data(fn, M, H, 3 * A, dqkv, w_qkv, dy1, ws, ws_bytes, stream);
+}
+
+int enc_packed_qkv_bwd_data(int tokens, int H, int width, const enc_bf16 *dqkv, const enc_bf16 *w_qkv, enc_bf16 *dy1,
+                            void *ws, size_t ws_bytes, enc_stream_t stream) {
+  const char *fn = "enc_packed_qkv_bwd_data";
+  if (int r = linear_dims(fn, tokens, {H, width})) return r;
+  return qkv_bwd_data(fn, tokens, H, width, dqkv, w_qkv, dy1, ws, ws_bytes, stream);
 }
 
 int enc_qkv_bwd_data_add(int M, int H, int A, const enc_bf16 *dqkv, const enc_bf16 *w_qkv, const enc_bf16 *addend,

@@ -559,3 +559,9 @@ def test_packed_layer(heads, kv, d, act):
         assert max_rel(f64(got), ref) < TOL_ACT, n
     for n, got, ref in [("dgu", dgu, DGU), ("dqkv", dqkv, DQKV), ("dx", dx, DX)] + [(n, gr[n], G[n]) for n in shapes]:
         assert max_rel(f64(got), ref) < TOL_GRAD, n
+
+
+@pytest.mark.parametrize("heads,kv,d,act", [(8, 1, 64, "silu"), (12, 4, 80, "gelu"), (4, 2, 128, "silu")])
+def test_packed_layer_whose_qkv_is_no_multiple_of_3_wide(heads, kv, d, act):
+    assert (heads + 2 * kv) % 3
+    test_packed_layer(heads, kv, d, act)

@@ -89,6 +89,24 @@ def test_plans_of_more_rows_than_attention_takes_are_refused():
             assert _st(name, *args) == B.ENC_OK, B.lib().enc_last_error()
 
 
+@no_gpu_only
+def test_projection_refusals():
+    fwd = [16, 64, 640, P, P, P, P, S0, 0, S0]  # eight query heads and one key and value head of 64
+    bwd = [16, 64, 640, P, P, P, S0, 0, S0]
+    for name, base, optional in (("enc_packed_qkv_fwd", fwd, (5,)), ("enc_packed_qkv_bwd_data", bwd, ())):
+        _bad(name, base, [(0, 0, INV), (1, 0, INV), (2, -8, INV), (1, 60, UNS), (2, 644, UNS), (0, 2 ** 31 // 640 + 1, UNS)])
+        _pointers(name, base, optional)
+        big = list(base)
+        big[0], big[1], big[2] = 64, 1024, 1280
+        at = len(base) - 3
+        need = B.linear_workspace_bytes(64, *((1280, 1024) if at == 7 else (1024, 1280)))
+        big[at], big[at + 1] = P, need - 1
+        assert need > 0 and _st(name, *big) == WSP
+        if STUB:  # (the product library would launch on fake pointers)
+            big[at + 1] = need
+            assert _st(name, *big) == _st(name, *base) == B.ENC_OK, B.lib().enc_last_error()
+
+
 def test_plan_sizes():
     # a header and one 16-byte item per 128 rows and sequence
     for tokens, seqs in ((1, 1), (128, 1), (129, 7), (100000, 40), (2 ** 31 - 1, 65536)):
