@@ -90,12 +90,9 @@ def test_forward_on_the_small_tile(steps, more):
         _forward(M, 64 * steps + more, F, "gelu" if (i + steps) % 2 else "silu", bias=i % 3 != 0, save=i != 2, seed=100 * i)
 
 
-@gpu
-@pytest.mark.parametrize("product,M,H,F,act", [(*c, act) for c in SPLIT for act in ACTS
-                                               if c[0] != B.GLU_UP_BWD_DATA or act == "silu"])  # (without one, that is)
-def test_every_number_of_parts(product, M, H, F, act):
-    """The workspace of every number of parts down to none: within the oracle's bounds,
-    and nothing written behind the workspace or the outputs."""
+def _in_parts(product, M, H, F, act, rooms):
+    """With workspaces for these numbers of parts: within the oracle's bounds, and nothing
+    written behind the workspace or the outputs."""
     N, K = _dims(product, M, H, F)
     x, w = random_bf16((M, K), 1), random_bf16((N, K) if product == B.GLU_UP_FWD else (K, N), 2, 1.5 / K ** 0.5)
     if product == B.GLU_UP_FWD:
@@ -111,7 +108,7 @@ def test_every_number_of_parts(product, M, H, F, act):
         ref, err = f64(x) @ f64(w), (K + 4) * P.FP32 * (np.abs(f64(x)) @ np.abs(f64(w)))
         refs = [(ref, P.BF16 * (np.abs(ref) + err) + err)]
     gx, gw = cuda(x), cuda(w)
-    for room in range(B.glu_plan(product, M, H, F)[2], -1, -1):
+    for room in rooms:
         size = max(4 * M * N * room, 16)
         parts = B.glu_plan(product, M, H, F, size)[2]
         announce(f"gated product {product} M={M} H={H} F={F} {act} workspace for {room} parts: {parts}")
@@ -131,3 +128,26 @@ def test_every_number_of_parts(product, M, H, F, act):
         # the partials are where the plan says: parts of them, and none unsplit
         used = 0 if parts == 1 else 4 * M * N * parts
         assert (ws[used:] == 0x7f).all() and (parts == 1 or not (ws[:used] == 0x7f).all())
+
+
+@gpu
+@pytest.mark.parametrize("product,M,H,F,act", [(*c, act) for c in SPLIT for act in ACTS
+                                               if c[0] != B.GLU_UP_BWD_DATA or act == "silu"])  # (without one, that is)
+def test_every_number_of_parts(product, M, H, F, act):
+    """From the whole workspace down to none."""
+    _in_parts(product, M, H, F, act, range(B.glu_plan(product, M, H, F)[2], -1, -1))
+
+
+@gpu
+@pytest.mark.parametrize("product,M,H,F,room,tile", [
+    (B.GLU_UP_FWD, 40, 3408, 208, 3, (64, 64)), (B.GLU_UP_FWD, 136, 3984, 1368, 4, (64, 128)),
+    (B.GLU_UP_FWD, 129, 3544, 1424, 4, (64, 192)), (B.GLU_UP_FWD, 61, 3496, 128, 6, (128, 128)),
+    (B.GLU_DOWN_BWD_DATA, 36, 3208, 272, 2, (64, 64)), (B.GLU_DOWN_BWD_DATA, 679, 3624, 528, 4, (64, 128)),
+    (B.GLU_DOWN_BWD_DATA, 717, 3728, 1408, 2, (64, 192)), (B.GLU_DOWN_BWD_DATA, 252, 5656, 160, 10, (128, 128)),
+    (B.GLU_UP_BWD_DATA, 36, 536, 2384, 4, (64, 64)), (B.GLU_UP_BWD_DATA, 51, 4464, 1832, 6, (64, 128)),
+    (B.GLU_UP_BWD_DATA, 86, 4768, 2760, 4, (64, 192)), (B.GLU_UP_BWD_DATA, 56, 1240, 1832, 7, (128, 128))])
+def test_every_tile_of_a_split(product, M, H, F, room, tile):
+    N, _ = _dims(product, M, H, F)
+    plan = B.glu_plan(product, M, H, F, 4 * M * N * room)
+    assert plan[:2] == tile and plan[2] > 1
+    _in_parts(product, M, H, F, "silu" if M % 2 else "gelu", [room])
