@@ -23,16 +23,20 @@
 //    accumulators, with no atomics and always in the same order.
 //
 // What bounds it: the matrix cores under the card's power limit on long sequences
-// (16 heads of 128 over 7936 + 515 + 1 tokens: busy 0.59 of the time at 1.8 GHz in
-// the forward, 0.67 at 1.7 in dQ, 0.61 at 1.85 in dK/dV), with as many LDS bytes
+// (16 heads of 128 over 7936 + 515 + 1 tokens: busy 0.58 of the time at 1.8 GHz in
+// the forward, 0.66 at 1.7 in dQ, 0.62 at 1.8 in dK/dV), with as many LDS bytes
 // as the LDS can deliver beside them (each 32x32x16 product reads 1 KB, which takes
 // the CU as long as its four SIMDs take to use it).  On short and ragged ones (40
-// images of 68 to 1020 tokens, 16 heads of 80: 0.32 to 0.37 busy at 2.05 GHz) the
-// latency of one wave's chain of products, exponentials and LDS reads, with the
-// workgroups' starts, ends and half-empty last tiles; below some 200 tokens each
-// kernel is bound by its bytes (112 x 128 tokens, 16 heads of 80: forward 31 us for
-// 147 MB, backward 97 for 441).  Figures beside the kernels are medians of a kernel
-// trace; rates count 4, 6 and 8 flops per query, key and element of a head in the
+// images of 68 to 1020 tokens, 16 heads of 80, at 2.0 GHz) the matrix cores are busy
+// 0.33 to 0.36 of the time and the vector units 0.53 (forward), 0.42 (dQ) and 0.35.
+// In the forward that is most of it: a wave's tile takes 320 cycles of products, but
+// 16 exponentials and 120 other vector instructions, which take a SIMD 520 (10 and 3
+// each in loops of their own), and the two overlap little.  The rest waits: a
+// workgroup has 18 tiles on average, before which nothing hides its work item, its
+// queries and its first tiles (waves past a sequence's end idle for 6% of the tiles).
+// Below some 200 tokens each kernel is bound by its bytes (112 x 128 tokens, 16 heads
+// of 80: forward 31 us for 147 MB, backward 97 for 441).  Figures beside the kernels
+// are medians of a kernel trace; rates count 4, 6 and 8 flops per query, key and element of a head in the
 // forward, dQ (S, dP and dQ) and dK/dV (S, dP, dV and dK).
 #include <float.h>
 #include <math.h>
@@ -282,7 +286,10 @@ struct Result {
     }
   }
   // += X^T s, s a 32x32 result [token of the tile][token], X the tile at base.
-  // s is rounded to bf16 here, the matrix cores' operand.
+  // s (P, or dS) is rounded to bf16 here: the other operand is bf16, and matrix
+  // instructions that take fp32 run at a sixteenth of the rate.  A weight is off by up
+  // to 2^-8 of itself, and the sums of the forward (l, and the lse) are of the unrounded
+  // ones; o is off by 2.0 to 2.6e-3 (2-norm, relative) where rounding o alone is 1.7e-3.
   template <class Reads>
   __device__ __forceinline__ void add(const Reads &rd, int base, const f32x16_t &s) {
     bf16x8_t b[2];
@@ -339,9 +346,9 @@ struct Result {
 // the vector units 0.45.)  Tile t + 2's keys and tile t + 1's values are loaded
 // meanwhile.
 //
-// 16 heads of 128 over 7936 + 515 + 1 tokens 473 us (1100 TFLOP/s); 16 of 80 over
-// the 40 images 69 (670); 32 of 128 on 8, causal, 24 prompts of 30 to 1625 tokens
-// 141 (700; 118 in a loop of this kernel alone).  A tile's loads, LDS reads and
+// 16 heads of 128 over 7936 + 515 + 1 tokens 484 us (1070 TFLOP/s); 16 of 80 over
+// the 40 images 71 (660); 32 of 128 on 8, causal, 24 prompts of 30 to 1625 tokens
+// 143 (690; 118 to 130 in a loop of this kernel alone).  A tile's loads, LDS reads and
 // exponentials, each left out of a copy, took 18, 61 and 13 us of 523 at 8192
 // tokens: none alone is what it waits for.
 
@@ -526,7 +533,7 @@ packed_fwd_kernel(PackedAttnArgs p) {
 // dS(t) = P (dP - D), and dQ^T += K^T dS^T follows.  Three stages of K (tile t
 // for dQ, t + 1 for S, t + 2 in flight) and two of V.
 //
-// The three sets as for the forward: 651 us (1190 TFLOP/s), 97 (720), 200 (730).
+// The three sets as for the forward: 665 us (1170 TFLOP/s), 99 (710), 203 (720).
 // It also leaves -lse sqrt(D) and -D_i for the dK/dV kernel.
 
 template <int D, int WPE>
@@ -667,8 +674,9 @@ packed_bwd_dq_kernel(PackedAttnArgs p) {
 // dP start from the dQ kernel's -lse sqrt(D) and -D_i, which lie in LDS in the
 // order of the result's registers, so neither is subtracted afterwards.
 //
-// The three sets as for the forward: 878 us (1180 TFLOP/s), 125 (740), 287 (680;
-// its longest workgroup takes 204 tiles in turn, four heads' 51).  64 keys
+// The three sets as for the forward: 897 us (1160 TFLOP/s), 128 (730), 293 (670;
+// its longest workgroup takes 204 tiles in turn, four heads' 51, where all of them
+// spread over the 512 that run at a time would be 106 each).  64 keys
 // per wave, which would halve the LDS reads, leave one wave per SIMD and were
 // slower; so was V in registers at D = 128 (spills).  Query tiles from the last
 // down, which all of a sequence's workgroups would read together, gave nothing.

@@ -117,6 +117,21 @@ def test_plan_lists_every_tile_longest_sequence_first(lens):
     assert np.array_equal(items, np.array(want).reshape(-1, 3))
 
 
+def test_plan_at_its_largest_size():
+    """As many rows as an attention call takes, nearly all in one sequence; the memory in
+    front of the plan and behind it stays as it was."""
+    tokens, n = (2 ** 31 - 1) // 192, 4096
+    announce(f"plan of {tokens} tokens")
+    size = B.packed_plan_bytes(tokens, 2)
+    buf = torch.full((size + 2 * n,), 0x5a, dtype=torch.uint8, device="cuda")
+    plan = buf[n:n + size]
+    B.enc_packed_plan(torch.tensor([0, 5, tokens], dtype=torch.int32, device="cuda"), tokens, plan)
+    items, tiles = _items(plan), -(-(tokens - 5) // 128)
+    want = [(5, tokens - 5, 128 * (tiles - 1 - k)) for k in range(tiles)] + [(0, 5, 0)]
+    assert np.array_equal(items, np.array(want))
+    assert (buf[:n] == 0x5a).all() and (buf[n + size:] == 0x5a).all()
+
+
 @pytest.mark.parametrize("cu", [[0, 700, 20, 900, 5, 1000], [-50, 10, 400], [0, 2000, 3000], [2 ** 31 - 1, -2 ** 31, 7]])
 def test_plan_of_bad_offsets_stays_inside_the_tensors(cu):
     announce(f"plan of offsets {cu}")
