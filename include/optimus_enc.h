@@ -553,7 +553,8 @@ enum enc_glu_act {
 
 /* The most workspace that the block's products (output [M, N], contraction K) make
  * use of: enc_linear_workspace_bytes where K is a multiple of 64, and where it is
- * not what splitting it takes.  A smaller one splits it into fewer parts. */
+ * not what splitting it takes.  With a smaller one tile and parts are chosen among
+ * those that it holds. */
 int enc_glu_workspace_bytes(int M, int N, int K, size_t *bytes);
 /* [Gated block step: both up-projections, the activation and the product]
  * y2 [M, H]; b_gu [2F] or NULL; h [M, F] bf16, from g and u in fp32; gu
